@@ -388,6 +388,85 @@ litevar_status litevar_windowed_attn_qkv8_fwd(const litevar_plan* plan, const in
                                               void* stream);
 
 /*
+ * K and V cache in 8 bits with one scale per block of tokens and head (Section 4's 8-bit K and V, for a cache that is
+ * written once and read at many steps; Q stays bf16).  The tokens of one (batch, head) are cut into segments -- the
+ * scales of a sequence (Section 2: s_k^2 tokens each), or one segment for an encoder's states -- and a segment into
+ * blocks of LITEVAR_KV8_BLOCK tokens counted from its first; no block spans two segments, so that storing scale by
+ * scale gives what storing all of them at once gives.
+ *   s = max |x| over the block's rows / 127,   code = clamp(rne(x / s), -127, 127) (0 where s = 0),   value = s * code
+ * Both quotients are correctly rounded binary32 quotients.
+ *   codes   DEVICE int8 [B, H, L, 64], 16-byte aligned, L = the sum of the segments
+ *   scales  DEVICE float [B, H, n_blocks], n_blocks = the sum of ceil(segment / LITEVAR_KV8_BLOCK)
+ *   segments, n_segments  HOST, token counts >= 0, at most LITEVAR_MAX_SCALES of them, fewer than 2^31 tokens in all
+ *
+ * litevar_kv8_blocks  out_first: HOST [n_segments + 1], the first block of every segment, then n_blocks.  Host-only.
+ * litevar_kv8_store   quantises the rows of the segments [segment_begin, segment_end) into the cache.
+ *     d_k, d_v     DEVICE [B, H, n, 64], n = the tokens of these segments; bf16 or fp32; finite
+ *     kv_strides   HOST, element strides of the (B, H, token) axes, multiples of 8; NULL = packed
+ *     d_len        optional DEVICE int32 [B]: tokens of the row's sequence, counted from the cache's first token, that
+ *                  count.  Rows from there on are not read, do not enter a scale and leave the cache as it was (they
+ *                  may hold anything).
+ * litevar_kv8_load    d_k_bf16, d_v_bf16 DEVICE bf16 [B, H, L, 64]: the rows of the segments [segment_begin,
+ *                     segment_end) as bf16(s * code); other rows are not written.
+ * litevar_windowed_attn_kv8_fwd
+ *                     litevar_windowed_attn_fwd on such a cache, whose segments are the plan's scales; only the scales
+ *                     that the plan's queries see have to be stored.  d_q, d_o DEVICE bf16 [B, H, q_len, 64] with
+ *                     strides as there; d_workspace DEVICE, 256-byte aligned, at least
+ *                     litevar_windowed_attn_kv8_workspace_bytes() bytes (NULL where that is 0), contents undefined
+ *                     before and after; calls that share a workspace must not overlap.  K and V reach the matrix
+ *                     products as bf16(s * code).  Other arguments as litevar_windowed_attn_fwd.
+ * All but litevar_kv8_blocks and the workspace size: asynchronous on `stream`.
+ */
+#define LITEVAR_KV8_BLOCK 64
+litevar_status litevar_kv8_blocks(const int32_t* segments, int32_t n_segments, int64_t* out_first);
+litevar_status litevar_kv8_store(const int32_t* segments, int32_t n_segments, int32_t segment_begin,
+                                 int32_t segment_end, const void* d_k, const void* d_v, litevar_dtype dt,
+                                 const int64_t* kv_strides, int32_t B, int32_t H, int32_t D, const int32_t* d_len,
+                                 int8_t* d_k8, float* d_k_scale, int8_t* d_v8, float* d_v_scale, void* stream);
+litevar_status litevar_kv8_load(const int32_t* segments, int32_t n_segments, int32_t segment_begin,
+                                int32_t segment_end, const int8_t* d_k8, const float* d_k_scale, const int8_t* d_v8,
+                                const float* d_v_scale, int32_t B, int32_t H, int32_t D, void* d_k_bf16,
+                                void* d_v_bf16, void* stream);
+litevar_status litevar_windowed_attn_kv8_workspace_bytes(const litevar_plan* plan, int32_t B, int32_t H,
+                                                         size_t* out_bytes);
+litevar_status litevar_windowed_attn_kv8_fwd(const litevar_plan* plan, const void* d_q, const int8_t* d_k8,
+                                             const float* d_k_scale, const int8_t* d_v8, const float* d_v_scale,
+                                             void* d_o, int32_t B, int32_t H, int32_t D, const int64_t* q_strides,
+                                             const int64_t* o_strides, float sm_scale, const uint8_t* d_cfg_share,
+                                             uint32_t flags, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Cross attention to an encoder's states, which a conditioned model of this kind has behind the self attention of every
+ * layer (no part of the paper's method):
+ *   O[b, h, i] = sum over t < len[b] of softmax_t(sm_scale * q_i . k_t) v_t,   zeros where len[b] = 0.
+ *   d_q, d_o    DEVICE [B, H, q_len, 64]; d_k, d_v DEVICE [B, H_kv, kv_len, 64], H a multiple of H_kv: query head h reads
+ *               kv head h / (H / H_kv).  q_len and kv_len may be 0 (K and V may then be NULL).  d_o must not overlap
+ *               the inputs.
+ *   dt          BF16: bf16 MFMA with fp32 accumulation, probabilities rounded to bf16 before P V.  F32: fp32 throughout.
+ *   strides     HOST, element strides of the (B, head, token) axes, multiples of 8, token stride >= 64; NULL = packed
+ *   d_kv_len    optional DEVICE int32 [B], taken as at least 0 and at most kv_len; NULL: kv_len for all.  K and V rows
+ *               from there on are not read.
+ *   d_workspace DEVICE, 16-byte aligned, at least litevar_cross_attn_workspace_bytes() bytes (NULL where that is 0),
+ *               contents undefined before and after; calls that share a workspace must not overlap
+ * litevar_cross_attn_kv8_fwd: the same with K and V in an 8-bit cache of one segment of kv_len tokens (see
+ *               litevar_kv8_store; the same lengths), Q and O in bf16.  The codes enter the matrix products exactly, the
+ *               scales are applied to fp32 sums.
+ * Inputs must be finite.  Results do not depend on the run (no atomics).  Asynchronous on `stream`.
+ */
+litevar_status litevar_cross_attn_workspace_bytes(int32_t B, int32_t H, int32_t H_kv, int32_t q_len, int32_t kv_len,
+                                                  size_t* out_bytes);
+litevar_status litevar_cross_attn_fwd(const void* d_q, const void* d_k, const void* d_v, void* d_o, int32_t B,
+                                      int32_t H, int32_t H_kv, int32_t q_len, int32_t kv_len, int32_t D,
+                                      litevar_dtype dt, const int64_t* q_strides, const int64_t* kv_strides,
+                                      const int64_t* o_strides, const int32_t* d_kv_len, float sm_scale,
+                                      void* d_workspace, size_t workspace_bytes, void* stream);
+litevar_status litevar_cross_attn_kv8_fwd(const void* d_q, const int8_t* d_k8, const float* d_k_scale,
+                                          const int8_t* d_v8, const float* d_v_scale, void* d_o, int32_t B, int32_t H,
+                                          int32_t H_kv, int32_t q_len, int32_t kv_len, int32_t D,
+                                          const int64_t* q_strides, const int64_t* o_strides, const int32_t* d_kv_len,
+                                          float sm_scale, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Diagnostics for benchmark reports (measurement, Section 4's efficiency figures are quoted
  * against what the hardware delivers): litevar_peak_copy enqueues a streaming copy of `bytes`
  * bytes (DEVICE pointers, 16-byte aligned, size a multiple of 16; HBM traffic = 2 x bytes);

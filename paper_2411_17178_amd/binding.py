@@ -85,9 +85,15 @@ def load_library():
                  "litevar_window_calibrate_static", "litevar_window_calibrate_band_workspace_bytes",
                  "litevar_window_calibrate_band", "litevar_peak_copy", "litevar_peak_read", "litevar_peak_mfma_bf16", "litevar_qkv8_quantize",
                  "litevar_qkv8_dequantize", "litevar_windowed_attn_qkv8_workspace_bytes",
-                 "litevar_windowed_attn_qkv8_fwd"):
+                 "litevar_windowed_attn_qkv8_fwd", "litevar_kv8_blocks", "litevar_kv8_store", "litevar_kv8_load",
+                 "litevar_windowed_attn_kv8_workspace_bytes", "litevar_windowed_attn_kv8_fwd",
+                 "litevar_cross_attn_workspace_bytes", "litevar_cross_attn_fwd", "litevar_cross_attn_kv8_fwd"):
         getattr(lib, name).restype = C.c_int32
     lib.attn_fwd = _ATTN_FWD(("litevar_windowed_attn_fwd", lib))
+    lib.kv8_store = _KV8_STORE(("litevar_kv8_store", lib))
+    lib.attn_kv8_fwd = _ATTN_KV8_FWD(("litevar_windowed_attn_kv8_fwd", lib))
+    lib.cross_attn_fwd = _CROSS_ATTN_FWD(("litevar_cross_attn_fwd", lib))
+    lib.cross_attn_kv8_fwd = _CROSS_ATTN_KV8_FWD(("litevar_cross_attn_kv8_fwd", lib))
     _lib = lib
     return lib
 
@@ -476,6 +482,231 @@ def litevar_windowed_attn_qkv8_fwd(plan, q8, q_sz, k8, k_sz, v8, v_sz, sm_scale,
         C.c_float(sm_scale), share_ptr, C.c_uint32(flags), C.c_void_p(workspace.data_ptr()),
         C.c_size_t(workspace.numel() * workspace.element_size()), _stream_handle(stream)))
     return out
+
+
+KV8_BLOCK = 64
+_KV8_STORE = C.CFUNCTYPE(C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32,
+                         C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                         C.c_void_p, C.c_void_p)
+_ATTN_KV8_FWD = C.CFUNCTYPE(C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                            C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_uint32,
+                            C.c_void_p, C.c_size_t, C.c_void_p)
+_CROSS_ATTN_FWD = C.CFUNCTYPE(C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
+                              C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                              C.c_float, C.c_void_p, C.c_size_t, C.c_void_p)
+_CROSS_ATTN_KV8_FWD = C.CFUNCTYPE(C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                  C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                  C.c_void_p, C.c_float, C.c_void_p, C.c_size_t, C.c_void_p)
+
+
+def _on_device(device, stream):
+    """Context in which calls and allocations go to `device` and to `stream` (None: that device's current stream): its
+    address, and a context manager or None where both already are the current ones."""
+    if stream is not None:
+        return stream.cuda_stream, torch.cuda.stream(stream)
+    address = torch.cuda.current_stream(device).cuda_stream
+    return address, None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _call(context, fn):
+    if context is None:
+        return fn()
+    with context:
+        return fn()
+
+
+def _check_lens(lens, B, device):
+    if lens is None:
+        return None
+    assert lens.dtype == torch.int32 and lens.shape == (B,) and lens.is_contiguous() and lens.device == device, \
+        "lens: contiguous int32 [B] on the operands' device"
+    return lens.data_ptr()
+
+
+def _workspace(workspace, need, device):
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    assert workspace.device == device and workspace.is_contiguous()
+    return workspace
+
+
+def litevar_kv8_blocks(segments):
+    """[first block of segment 0, ..., of the last one, number of blocks] of an 8-bit cache with these token counts."""
+    n = len(segments)
+    out = (C.c_int64 * (n + 1))()
+    _check(load_library().litevar_kv8_blocks((C.c_int32 * n)(*[int(s) for s in segments]), C.c_int32(n), out))
+    return [int(x) for x in out]
+
+
+class KV8Cache:
+    """K and V of a layer as 8-bit codes [B, H, L, 64] with one float32 scale per block of 64 tokens and head,
+    [B, H, n_blocks].  `segments`: the token counts that the blocks are counted in (a sequence's scales, s * s each; one
+    for an encoder's states)."""
+
+    def __init__(self, segments, k8, k_scale, v8, v_scale):
+        self.segments = [int(s) for s in segments]
+        self.first_block = litevar_kv8_blocks(self.segments)
+        assert k8.is_cuda and k8.dim() == 4 and k8.shape[2] == sum(self.segments) and k8.shape[3] == 64
+        self.B, self.H, self.kv_len = k8.shape[:3]
+        scale_shape = (self.B, self.H, self.first_block[-1])
+        for codes, scale in ((k8, k_scale), (v8, v_scale)):
+            assert codes.dtype == torch.int8 and codes.shape == k8.shape and codes.is_contiguous() and codes.device == k8.device
+            assert scale.dtype == torch.float32 and scale.shape == scale_shape and scale.is_contiguous() and scale.device == k8.device
+        self.k8, self.k_scale, self.v8, self.v_scale = k8, k_scale, v8, v_scale
+        self.device = k8.device
+        self._segments = (C.c_int32 * len(self.segments))(*self.segments)
+        self.offsets = [0]
+        for s in self.segments:
+            self.offsets.append(self.offsets[-1] + s)
+
+    def _pointers(self):
+        return self.k8.data_ptr(), self.k_scale.data_ptr(), self.v8.data_ptr(), self.v_scale.data_ptr()
+
+
+def litevar_kv8_cache(segments, B, H, device="cuda"):
+    """An 8-bit cache with nothing stored in it."""
+    blocks, L = litevar_kv8_blocks(segments)[-1], sum(int(s) for s in segments)
+    codes = [torch.empty((B, H, L, 64), dtype=torch.int8, device=device) for _ in range(2)]
+    scales = [torch.zeros((B, H, blocks), dtype=torch.float32, device=device) for _ in range(2)]
+    return KV8Cache(segments, codes[0], scales[0], codes[1], scales[1])
+
+
+def litevar_kv8_store(cache, k, v, segments=None, lens=None, stream=None):
+    """Quantise k, v [B, H, n, 64] (bf16 or fp32) into the cache's segments [begin, end) (default: all of them).
+    lens: optional int32 CUDA tensor [B], the tokens of each row's sequence that count, from the cache's first."""
+    begin, end = (0, len(cache.segments)) if segments is None else segments
+    assert 0 <= begin < end <= len(cache.segments)
+    dt = _DTYPES.get(k.dtype)
+    if dt is None or v.dtype != k.dtype:
+        raise TypeError(f"unsupported dtypes {k.dtype}, {v.dtype}")
+    assert k.device == v.device == cache.device
+    B, H = cache.B, cache.H
+    assert k.shape == v.shape == (B, H, cache.offsets[end] - cache.offsets[begin], 64)
+    assert k.stride() == v.stride(), "k and v must share strides"
+    lens_ptr = _check_lens(lens, B, cache.device)
+    address, context = _on_device(cache.device, stream)
+    k8, k_scale, v8, v_scale = cache._pointers()
+    fn = load_library().kv8_store
+    rc = _call(context, lambda: fn(cache._segments, len(cache.segments), begin, end, k.data_ptr(), v.data_ptr(), dt, _strides(k),
+                                   B, H, 64, lens_ptr, k8, k_scale, v8, v_scale, address))
+    if rc != 0:
+        _check(rc)
+    return cache
+
+
+def litevar_kv8_load(cache, segments=None, out=None, stream=None):
+    """(k, v): the rows of the cache's segments [begin, end) (default: all) as bf16 [B, H, L, 64]; other rows are not
+    written.  out: optional pair of such tensors."""
+    begin, end = (0, len(cache.segments)) if segments is None else segments
+    address, context = _on_device(cache.device, stream)
+    if out is None:
+        out = _call(context, lambda: tuple(torch.empty(cache.k8.shape, dtype=torch.bfloat16, device=cache.device) for _ in range(2)))
+        context = _on_device(cache.device, stream)[1]
+    for t in out:
+        assert t.device == cache.device and t.dtype == torch.bfloat16 and t.shape == cache.k8.shape and t.is_contiguous()
+    k8, k_scale, v8, v_scale = (C.c_void_p(p) for p in cache._pointers())
+    _check(_call(context, lambda: load_library().litevar_kv8_load(
+        cache._segments, C.c_int32(len(cache.segments)), C.c_int32(begin), C.c_int32(end), k8, k_scale, v8, v_scale,
+        C.c_int32(cache.B), C.c_int32(cache.H), C.c_int32(64), C.c_void_p(out[0].data_ptr()), C.c_void_p(out[1].data_ptr()),
+        C.c_void_p(address))))
+    return out
+
+
+def litevar_windowed_attn_kv8_workspace_bytes(plan, B, H):
+    n = C.c_size_t(0)
+    _check(load_library().litevar_windowed_attn_kv8_workspace_bytes(C.byref(plan.handle), C.c_int32(B), C.c_int32(H), C.byref(n)))
+    return n.value
+
+
+def litevar_windowed_attn_kv8_fwd(plan, q, cache, sm_scale, out=None, cfg_share=None, workspace=None, stream=None):
+    """Windowed attention of q [B, H, q_len, 64] (bf16) on an 8-bit cache whose segments are the plan's scales (those
+    that the plan's queries see have been stored).  workspace: an uint8 CUDA tensor of
+    litevar_windowed_attn_kv8_workspace_bytes() bytes (allocated per call when omitted)."""
+    handle = plan.handle
+    if q.dtype != torch.bfloat16:
+        raise TypeError(f"unsupported dtype {q.dtype}")
+    assert q.device == cache.device
+    B, H, Lq, D = shape = q.shape
+    assert Lq == handle.q_len and (B, H, D) == (cache.B, cache.H, 64)
+    assert len(cache.segments) == handle.n_scales and all(s == handle.scales[i] ** 2 for i, s in enumerate(cache.segments)), \
+        "the cache's segments must be the plan's scales"
+    flags, share_ptr = 0, None
+    if cfg_share is not None:
+        assert cfg_share.device == q.device and cfg_share.dtype == torch.uint8 and cfg_share.is_contiguous()
+        assert cfg_share.shape == (H, handle.n_scales)
+        flags, share_ptr = FLAG_CFG_SHARE, cfg_share.data_ptr()
+    address, context = _on_device(q.device, stream)
+    k8, k_scale, v8, v_scale = cache._pointers()
+    fn = load_library().attn_kv8_fwd
+
+    def call():
+        o = torch.empty_like(q) if out is None else out
+        assert o.shape == shape and o.dtype == q.dtype and o.device == q.device
+        need = litevar_windowed_attn_kv8_workspace_bytes(plan, B, H)
+        w = _workspace(workspace, need, q.device) if need else None
+        rc = fn(C.addressof(handle), q.data_ptr(), k8, k_scale, v8, v_scale, o.data_ptr(), B, H, D, _strides(q), _strides(o),
+                sm_scale, share_ptr, flags, w.data_ptr() if need else None, w.numel() * w.element_size() if need else 0, address)
+        if rc != 0:
+            _check(rc)
+        return o
+    return _call(context, call)
+
+
+def litevar_cross_attn_workspace_bytes(B, H, H_kv, q_len, kv_len):
+    n = C.c_size_t(0)
+    _check(load_library().litevar_cross_attn_workspace_bytes(C.c_int32(B), C.c_int32(H), C.c_int32(H_kv), C.c_int32(q_len),
+                                                             C.c_int32(kv_len), C.byref(n)))
+    return n.value
+
+
+def _cross_attn(q, H_kv, kv_len, lens, out, workspace, stream, call):
+    B, H, q_len, D = shape = q.shape
+    lens_ptr = _check_lens(lens, B, q.device)
+    address, context = _on_device(q.device, stream)
+
+    def run():
+        o = torch.empty_like(q) if out is None else out
+        assert o.shape == shape and o.dtype == q.dtype and o.device == q.device
+        need = litevar_cross_attn_workspace_bytes(B, H, H_kv, q_len, kv_len)
+        w = _workspace(workspace, need, q.device) if need else None
+        rc = call(o, lens_ptr, w.data_ptr() if need else None, w.numel() * w.element_size() if need else 0, address)
+        if rc != 0:
+            _check(rc)
+        return o
+    return _call(context, run)
+
+
+def litevar_cross_attn_fwd(q, k, v, sm_scale, lens=None, out=None, workspace=None, stream=None):
+    """out[B, H, q_len, 64] = attention of q to the first lens[b] (default: all) of the kv_len rows of k, v
+    [B, H_kv, kv_len, 64], H a multiple of H_kv; zeros where lens[b] is 0.  bf16 or fp32.  lens: int32 CUDA tensor [B].
+    workspace: an uint8 CUDA tensor of litevar_cross_attn_workspace_bytes() bytes (allocated per call when omitted)."""
+    dt = _DTYPES.get(q.dtype)
+    if dt is None or k.dtype != q.dtype or v.dtype != q.dtype:
+        raise TypeError(f"unsupported dtypes {q.dtype}, {k.dtype}, {v.dtype}")
+    assert q.is_cuda and k.device == v.device == q.device
+    B, H, q_len, D = q.shape
+    assert k.dim() == 4 and k.shape[0] == B and k.shape[3] == D and v.shape == k.shape
+    assert k.stride() == v.stride(), "k and v must share strides"
+    H_kv, kv_len = k.shape[1], k.shape[2]
+    fn = load_library().cross_attn_fwd
+    return _cross_attn(q, H_kv, kv_len, lens, out, workspace, stream, lambda o, lens_ptr, w, w_bytes, address: fn(
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), B, H, H_kv, q_len, kv_len, D, dt, _strides(q), _strides(k),
+        _strides(o), lens_ptr, sm_scale, w, w_bytes, address))
+
+
+def litevar_cross_attn_kv8_fwd(q, cache, sm_scale, lens=None, out=None, workspace=None, stream=None):
+    """litevar_cross_attn_fwd on an 8-bit cache of one segment; q bf16."""
+    if q.dtype != torch.bfloat16:
+        raise TypeError(f"unsupported dtype {q.dtype}")
+    assert q.device == cache.device
+    B, H, q_len, D = q.shape
+    assert B == cache.B and D == 64
+    assert len(cache.segments) == 1, "cross attention reads a cache of one segment"
+    fn = load_library().cross_attn_kv8_fwd
+    k8, k_scale, v8, v_scale = cache._pointers()
+    return _cross_attn(q, cache.H, cache.kv_len, lens, out, workspace, stream, lambda o, lens_ptr, w, w_bytes, address: fn(
+        q.data_ptr(), k8, k_scale, v8, v_scale, o.data_ptr(), B, H, cache.H, q_len, cache.kv_len, D, _strides(q), _strides(o),
+        lens_ptr, sm_scale, w, w_bytes, address))
 
 
 def litevar_peak_copy(src, dst, stream=None):

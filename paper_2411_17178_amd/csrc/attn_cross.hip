@@ -1,0 +1,441 @@
+// Cross attention for gfx950 (CDNA4): every query row sees the first len[b] of kv_len keys (an encoder's states),
+//   O[b, h, i] = sum over t < len[b] of softmax_t(sm q_i . k_t) v_t,
+// with K and V rows in bf16, in fp32, or as 8-bit codes with one scale per block of 64 tokens and kv head.  Query
+// head h reads kv head h / (H / H_kv): the rows of one kv head are its G = H / H_kv query heads' rows, head after head.
+//
+// One workgroup = four waves = 32 rows of one (batch, kv head) and one part of the key axis; the waves take the part's
+// blocks of 64 keys (32 in fp32) in turn and join their results through LDS.  With several parts, each leaves its sums
+// in the workspace and a second launch joins them.
+#include <cstring>
+
+#include "attn_bf16_common.h"
+
+namespace lv {
+namespace {
+
+constexpr int kRows = 32;                      // rows per workgroup: the columns of a 32 x 32 tile
+constexpr int kWaves = 4;
+constexpr int kBlock = LITEVAR_KV8_BLOCK;      // keys per turn
+constexpr int kPitch = 68;                     // floats per row of the joining buffer
+
+enum Kind { kBf16 = 0, kF32 = 1, kCodes = 2 };
+
+struct CrossArgs {
+  const void* q; const void* k; const void* v; void* o;
+  const float* k_scale; const float* v_scale;  // codes: [B][H_kv][blocks]
+  int64_t qs[3], ks[3], os[3];                 // element strides of (B, head, token)
+  const int32_t* len;                          // [B] or nullptr
+  int B, H, Hkv, G, q_len, kv_len;
+  int rows, tiles;                             // rows of a kv head, tiles of 32 of them
+  int parts;                                   // of the key axis
+  int scale_blocks;                            // of a (batch, kv head)
+  uint32_t q_magic, tiles_magic, hkv_magic, parts_magic;   // see divmod_by
+  uint32_t first_block;
+  float* part_o; float2* part_ml;              // [item][32][64] and [item][32] (largest score, sum), item = workgroup
+};
+
+struct Row { int h, i; };                      // query head, token
+
+__device__ inline Row row_at(const CrossArgs& a, int j, int r) {
+  int g, i;
+  divmod_by((uint32_t)r, (uint32_t)a.q_len, a.q_magic, g, i);
+  return Row{j * a.G + g, i};
+}
+
+__device__ inline int keys_of(const CrossArgs& a, int b) { return a.len ? min(max(a.len[b], 0), a.kv_len) : a.kv_len; }
+
+__device__ inline unsigned swizzle(unsigned r) { return ((r & 3u) << 1) | ((r >> 2) & 1u); }
+
+// eight codes (a word pair) as bf16, exactly
+__device__ inline bf16x8 codes_to_bf16(unsigned lo, unsigned hi) {
+  bf16x8 r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = (__bf16)(float)(int8_t)(((e < 4 ? lo : hi) >> (8 * (e & 3))) & 0xffu);
+  return r;
+}
+
+// Writes eight output values of row r, dims 8 part .. + 7.
+template <int KIND> __device__ inline void store_row(const CrossArgs& a, int b, int j, int r, int part, const float (&x)[8]) {
+  const Row w = row_at(a, j, r);
+  const int64_t at = b * a.os[0] + w.h * a.os[1] + w.i * a.os[2] + 8 * part;
+  if constexpr (KIND == kF32) {
+    float* p = (float*)a.o + at;
+    *(float4*)p = make_float4(x[0], x[1], x[2], x[3]);
+    *(float4*)(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+  } else {
+    bf16x8 y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = (__bf16)x[e];
+    *(bf16x8*)((__bf16*)a.o + at) = y;
+  }
+}
+
+// Joins `n` sums of 32 rows: sum s has its rows' (largest score, sum) at ml(s)[row] and its products at o(s)[row].
+// Thread t forms dims 8 (t / 32) .. of row t % 32.  Returns the joined largest score and sum; x is not divided.
+template <class Ml, class O>
+__device__ inline float2 join(int n, float c, Ml ml, O o, float (&x)[8]) {
+  float m = -INFINITY, l = 0.f;
+  for (int s = 0; s < n; ++s) m = fmaxf(m, ml(s).x);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = 0.f;
+  if (m == -INFINITY) return make_float2(m, 0.f);
+  for (int s = 0; s < n; ++s) {
+    const float2 p = ml(s);
+    if (p.x == -INFINITY) continue;            // (no key: nothing was written)
+    const float f = __builtin_amdgcn_exp2f((p.x - m) * c);
+    l = fmaf(p.y, f, l);
+    const float* y = o(s);
+    const float4 lo = *(const float4*)y, hi = *(const float4*)(y + 4);
+    x[0] = fmaf(lo.x, f, x[0]); x[1] = fmaf(lo.y, f, x[1]); x[2] = fmaf(lo.z, f, x[2]); x[3] = fmaf(lo.w, f, x[3]);
+    x[4] = fmaf(hi.x, f, x[4]); x[5] = fmaf(hi.y, f, x[5]); x[6] = fmaf(hi.z, f, x[6]); x[7] = fmaf(hi.w, f, x[7]);
+  }
+  return make_float2(m, l);
+}
+
+}  // namespace
+
+// S^T (32 keys x 32 rows) = K (A operand, straight from memory) . Q^T, so that a lane owns one row and 16 of 32 keys;
+// O^T (64 dims x rows) += V^T . P^T.  The order of the head dimensions inside the first product is free: lane half hh
+// takes dims 32 hh .. + 31, a lane's piece of a K row is then contiguous.  V^T is read from LDS by transposing reads
+// (bf16, codes) or straight from memory (fp32, a value per lane).  Softmax with the running largest score as the reference,
+// subtracted before the scale is applied, so that scores of any size keep their differences.
+template <int KIND>
+__global__ __launch_bounds__(kWaves * 64) void k_cross_rows(CrossArgs a, float c) {
+  __shared__ __align__(16) unsigned char smem[kWaves * kRows * kPitch * 4 + kWaves * kRows * 8];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int n = lane & 31, hh = lane >> 5;
+  int rest, tile, part, bj, b, j;
+  const uint32_t item = a.first_block + blockIdx.x;
+  divmod_by(item, (uint32_t)a.parts, a.parts_magic, rest, part);
+  divmod_by((uint32_t)rest, (uint32_t)a.tiles, a.tiles_magic, bj, tile);
+  divmod_by((uint32_t)bj, (uint32_t)a.Hkv, a.hkv_magic, b, j);
+  const int n_keys = keys_of(a, b);
+  const int row0 = tile * kRows;
+  const int r = min(row0 + n, a.rows - 1);     // (a column without a row holds the last one; it is not stored)
+  const Row qr = row_at(a, j, r);
+  const int64_t q_at = b * a.qs[0] + qr.h * a.qs[1] + qr.i * a.qs[2] + 32 * hh, kv_at = b * a.ks[0] + j * a.ks[1];
+
+  // this part's turns: blocks of kBlock keys
+  const int blocks = (n_keys + kBlock - 1) / kBlock;
+  const int begin = (int)((int64_t)blocks * part / a.parts), end = (int)((int64_t)blocks * (part + 1) / a.parts);
+
+  float m = -INFINITY, L = 0.f;                // the row's reference; this lane's share of the sum
+  f32x16 O[2] = {f32x16{}, f32x16{}};
+  // scores of 32 keys -> probabilities, with the reference moved to their largest
+  auto softmax = [&](f32x16& S, int key0) {
+    const int left = n_keys - key0 - 4 * hh;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      S[e] = 8 * (e >> 2) + (e & 3) < left ? S[e] : -INFINITY;
+      mx = fmaxf(mx, S[e]);
+    }
+    mx = fmaxf(mx, other_half(mx));
+    const float to = fmaxf(m, mx);
+    if (__builtin_amdgcn_ballot_w64(to > m) != 0) {
+      const float alpha = m > -INFINITY ? __builtin_amdgcn_exp2f((m - to) * c) : 1.f;
+      m = to; L *= alpha;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) { O[0][e] *= alpha; O[1][e] *= alpha; }
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) S[e] = __builtin_amdgcn_exp2f((S[e] - m) * c);
+  };
+
+  if constexpr (KIND == kF32) {
+    const float* q = (const float*)a.q + q_at;
+    float qf[32];
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      const float4 x = *(const float4*)(q + 4 * t);
+      qf[4 * t] = x.x; qf[4 * t + 1] = x.y; qf[4 * t + 2] = x.z; qf[4 * t + 3] = x.w;
+    }
+    const float* K = (const float*)a.k + kv_at + 32 * hh;
+    const float* V = (const float*)a.v + kv_at + n;
+    for (int key0 = kBlock * begin + 32 * wave; key0 < min(n_keys, kBlock * end); key0 += 32 * kWaves) {
+      const float* kp = K + (int64_t)min(key0 + n, n_keys - 1) * a.ks[2];
+      float kf[32];
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const float4 x = *(const float4*)(kp + 4 * t);
+        kf[4 * t] = x.x; kf[4 * t + 1] = x.y; kf[4 * t + 2] = x.z; kf[4 * t + 3] = x.w;
+      }
+      f32x16 S = f32x16{};
+#pragma unroll
+      for (int t = 0; t < 32; ++t) S = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[t], qf[t], S, 0, 0, 0);
+      softmax(S, key0);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int key = key0 + 8 * (e >> 2) + 4 * hh + (e & 3);
+        const float* vp = V + (int64_t)min(key, n_keys - 1) * a.ks[2];   // (probability 0 where the key is clamped)
+        L += S[e];
+        O[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(vp[0], S[e], O[0], 0, 0, 0);
+        O[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(vp[32], S[e], O[1], 0, 0, 0);
+      }
+    }
+  } else {
+    const __bf16* q = (const __bf16*)a.q + q_at;
+    bf16x8 qf[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) qf[t] = as_bf16x8(*(const uint4*)(q + 8 * t));
+    unsigned char* const Vs = smem + wave * 32 * 128;    // this wave's 32 V rows in bf16
+    const int64_t scale_at = KIND == kCodes ? (int64_t)bj * a.scale_blocks : 0;
+    for (int blk = begin + wave; blk < end; blk += kWaves) {
+      float ks = 1.f, vs = 1.f;
+      if constexpr (KIND == kCodes) { ks = a.k_scale[scale_at + blk]; vs = a.v_scale[scale_at + blk]; }
+#pragma unroll 1
+      for (int key0 = kBlock * blk; key0 < min(n_keys, kBlock * (blk + 1)); key0 += 32) {
+        const int64_t k_row = (int64_t)min(key0 + n, n_keys - 1) * a.ks[2];
+        f32x16 S = f32x16{};
+        if constexpr (KIND == kCodes) {
+          const u32x4* kp = (const u32x4*)((const int8_t*)a.k + kv_at + k_row + 32 * hh);
+          const u32x4 x0 = kp[0], x1 = kp[1];
+          S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(codes_to_bf16(x0[0], x0[1]), qf[0], S, 0, 0, 0);
+          S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(codes_to_bf16(x0[2], x0[3]), qf[1], S, 0, 0, 0);
+          S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(codes_to_bf16(x1[0], x1[1]), qf[2], S, 0, 0, 0);
+          S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(codes_to_bf16(x1[2], x1[3]), qf[3], S, 0, 0, 0);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) S[e] *= ks;
+          // V codes: four lanes per row, sixteen rows per load
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int row = 16 * i + (lane >> 2), key = key0 + row, p = 2 * (lane & 3);
+            const u32x4 x = *(const u32x4*)((const int8_t*)a.v + kv_at + (int64_t)min(key, n_keys - 1) * a.ks[2] + 8 * p);
+            const bf16x8 lo = codes_to_bf16(x[0], x[1]), hi = codes_to_bf16(x[2], x[3]);
+            *(bf16x8*)(Vs + row * 128 + (((unsigned)p ^ swizzle((unsigned)row)) << 4)) = lo;
+            *(bf16x8*)(Vs + row * 128 + (((unsigned)(p + 1) ^ swizzle((unsigned)row)) << 4)) = hi;
+          }
+        } else {
+          const __bf16* kp = (const __bf16*)a.k + kv_at + k_row + 32 * hh;
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+            S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(kp + 8 * t)), qf[t], S, 0, 0, 0);
+          // V: eight lanes per row, eight rows per load; a row behind the last key counts as the last one, with
+          // probability 0
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int row = 8 * i + (lane >> 3);
+            const uint4 x = *(const uint4*)((const __bf16*)a.v + kv_at + (int64_t)min(key0 + row, n_keys - 1) * a.ks[2] + 8 * (lane & 7));
+            *(uint4*)(Vs + row * 128 + ((((unsigned)lane & 7u) ^ swizzle((unsigned)row)) << 4)) = x;
+          }
+        }
+        softmax(S, key0);
+        asm volatile("" ::: "memory");         // (the rows of V are read by other lanes than wrote them; LDS keeps a wave's order)
+        bf16x8 pb[2];
+        float sum = L;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) pb[t][e] = (__bf16)S[8 * t + e];
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pb[t][e], pb[t][e + 1]}, kOnes, sum, false);
+        }
+        L = sum;
+        f32x16 P[2];
+        if constexpr (KIND == kCodes) { P[0] = f32x16{}; P[1] = f32x16{}; } else { P[0] = O[0]; P[1] = O[1]; }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int dt = 0; dt < 2; ++dt) {
+            s16x8 v8;
+#pragma unroll
+            for (int jj = 0; jj < 2; ++jj) {
+              const unsigned l16 = (unsigned)lane & 15u, row = 16u * t + 8u * jj + 4u * (unsigned)hh + (l16 >> 2);
+              const unsigned piece = 4u * dt + 2u * (((unsigned)lane >> 4) & 1u) + ((l16 & 3u) >> 1);
+              const s16x4 x = lds_read_tr16(Vs + row * 128 + ((piece ^ swizzle(row)) << 4) + 8u * (l16 & 1u));
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v8[4 * jj + e] = x[e];
+            }
+            P[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v8), pb[t], P[dt], 0, 0, 0);
+          }
+        asm volatile("" ::: "memory");
+        if constexpr (KIND == kCodes) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) { O[0][e] = fmaf(P[0][e], vs, O[0][e]); O[1][e] = fmaf(P[1][e], vs, O[1][e]); }
+        } else {
+          O[0] = P[0]; O[1] = P[1];
+        }
+      }
+    }
+  }
+
+  // ---- join the waves ----
+  L += other_half(L);
+  float2* const ML = (float2*)(smem + kWaves * kRows * kPitch * 4);
+  __syncthreads();                             // (the rows of V are read)
+  float* const mine = (float*)smem + (wave * kRows + n) * kPitch + 4 * hh;
+#pragma unroll
+  for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      *(float4*)(mine + 32 * dt + 8 * t) = make_float4(O[dt][4 * t], O[dt][4 * t + 1], O[dt][4 * t + 2], O[dt][4 * t + 3]);
+  if (hh == 0) ML[wave * kRows + n] = make_float2(m, L);
+  __syncthreads();
+  const int row = tid & 31, dims = tid >> 5;
+  float x[8];
+  const float2 ml = join(kWaves, c, [&](int s) { return ML[s * kRows + row]; },
+                         [&](int s) { return (const float*)smem + (s * kRows + row) * kPitch + 8 * dims; }, x);
+  if (a.parts > 1) {
+    if (dims == 0) a.part_ml[(int64_t)item * kRows + row] = ml;
+    float* p = a.part_o + ((int64_t)item * kRows + row) * 64 + 8 * dims;
+    *(float4*)p = make_float4(x[0], x[1], x[2], x[3]);
+    *(float4*)(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+    return;
+  }
+  if (row0 + row >= a.rows) return;
+  const float inv = ml.y > 0.f ? 1.f / ml.y : 0.f;       // (no key: zeros)
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] *= inv;
+  store_row<KIND>(a, b, j, row0 + row, dims, x);
+}
+
+// Joins the parts of one tile of rows: a workgroup per (batch, kv head, tile).
+template <int KIND>
+__global__ __launch_bounds__(256) void k_cross_join(CrossArgs a, float c) {
+  const int row = threadIdx.x & 31, dims = threadIdx.x >> 5;
+  int tile, bj, b, j;
+  const uint32_t at = a.first_block + blockIdx.x;
+  divmod_by(at, (uint32_t)a.tiles, a.tiles_magic, bj, tile);
+  divmod_by((uint32_t)bj, (uint32_t)a.Hkv, a.hkv_magic, b, j);
+  if (tile * kRows + row >= a.rows) return;
+  const int64_t first = (int64_t)at * a.parts;
+  float x[8];
+  const float2 ml = join(a.parts, c, [&](int s) { return a.part_ml[(first + s) * kRows + row]; },
+                         [&](int s) { return a.part_o + ((first + s) * kRows + row) * 64 + 8 * dims; }, x);
+  const float inv = ml.y > 0.f ? 1.f / ml.y : 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] *= inv;
+  store_row<KIND>(a, b, j, tile * kRows + row, dims, x);
+}
+
+namespace {
+
+// Parts of the key axis: as many as give about four workgroups per CU, none of fewer than four blocks.
+int parts_of(int64_t tiles, int64_t kv_len) {
+  const int64_t blocks = (kv_len + kBlock - 1) / kBlock;
+  int64_t p = tiles > 0 ? 1024 / tiles : 1;
+  if (p > blocks / kWaves) p = blocks / kWaves;
+  return (int)(p < 1 ? 1 : p);
+}
+
+uint32_t magic_of(int64_t n) { return (uint32_t)(((uint64_t)1 << 32) / (uint64_t)(n > 1 ? n : 1) - (n <= 1)); }
+
+litevar_status check_shape(int32_t B, int32_t H, int32_t H_kv, int32_t q_len, int32_t kv_len) {
+  if (B < 1 || H < 1 || H_kv < 1) return fail(LITEVAR_E_INVALID_ARG, "B, H and H_kv must be positive (got %d, %d, %d)", B, H, H_kv);
+  if (H % H_kv) return fail(LITEVAR_E_INVALID_ARG, "H = %d is not a multiple of H_kv = %d", H, H_kv);
+  if (q_len < 0 || kv_len < 0) return fail(LITEVAR_E_INVALID_ARG, "q_len and kv_len must not be negative (got %d, %d)", q_len, kv_len);
+  if ((int64_t)B * H > (1 << 24)) return fail(LITEVAR_E_UNSUPPORTED, "B*H above 2^24");
+  if ((int64_t)(H / H_kv) * q_len >= ((int64_t)1 << 31) - kRows || kv_len >= 0x7fffffff - 2 * kBlock)
+    return fail(LITEVAR_E_UNSUPPORTED, "2^31 rows of a kv head, or 2^31 keys, or more");
+  if ((int64_t)B * H_kv * (((int64_t)(H / H_kv) * q_len + kRows - 1) / kRows) >= 0x7fffffff)
+    return fail(LITEVAR_E_UNSUPPORTED, "grid too large");
+  return LITEVAR_OK;
+}
+
+int64_t tiles_of(int32_t B, int32_t H, int32_t H_kv, int32_t q_len) {
+  return (int64_t)B * H_kv * (((int64_t)(H / H_kv) * q_len + kRows - 1) / kRows);
+}
+
+// (the stride of an axis with one entry is never used, and is what it is)
+litevar_status strides_of(const int64_t* s, int B, int heads, int64_t n, int D, int64_t (&out)[3]) {
+  if (!s) { out[2] = D; out[1] = n * D; out[0] = heads * n * D; return LITEVAR_OK; }
+  out[0] = B > 1 ? s[0] : 0; out[1] = heads > 1 ? s[1] : 0; out[2] = n > 1 ? s[2] : D;
+  if (out[2] < D || out[2] % 8 || out[1] < 0 || out[0] < 0 || out[1] % 8 || out[0] % 8)
+    return fail(LITEVAR_E_INVALID_ARG, "strides must be non-negative multiples of 8 with token stride >= D");
+  return LITEVAR_OK;
+}
+
+template <int KIND> litevar_status launch(CrossArgs& a, float c, hipStream_t st) {
+  const int64_t tiles = (int64_t)a.B * a.Hkv * a.tiles;
+  if (litevar_status s = launch_in_parts(tiles * a.parts, kWaves * 64, "cross attention launch", [&](int64_t first, unsigned n) {
+        a.first_block = (uint32_t)first;
+        hipLaunchKernelGGL(k_cross_rows<KIND>, dim3(n), dim3(kWaves * 64), 0, st, a, c);
+      })) return s;
+  if (a.parts == 1) return LITEVAR_OK;
+  return launch_in_parts(tiles, 256, "cross attention join launch", [&](int64_t first, unsigned n) {
+    a.first_block = (uint32_t)first;
+    hipLaunchKernelGGL(k_cross_join<KIND>, dim3(n), dim3(256), 0, st, a, c);
+  });
+}
+
+// What both entry points check and fill; `kind` as in Kind.
+litevar_status cross_attention(CrossArgs& a, Kind kind, int32_t B, int32_t H, int32_t H_kv, int32_t q_len, int32_t kv_len, int32_t D,
+                               const int64_t* q_strides, const int64_t* kv_strides, const int64_t* o_strides, float sm_scale,
+                               void* d_workspace, size_t workspace_bytes, void* stream) {
+  if (litevar_status s = check_shape(B, H, H_kv, q_len, kv_len)) return s;
+  if (D != 64) return fail(LITEVAR_E_UNSUPPORTED, "head dimension %d is not supported (only 64)", D);
+  uint32_t bits;                               // (compared as bits: the build lets the compiler assume that no value is NaN)
+  memcpy(&bits, &sm_scale, sizeof bits);
+  if (bits == 0 || bits > 0x461c4000u)         // 1e4f; negative values, infinities and NaN are above it
+    return fail(LITEVAR_E_INVALID_ARG, "sm_scale must be finite, positive and at most 1e4");
+  if (litevar_status s = strides_of(q_strides, B, H, q_len, D, a.qs)) return s;
+  if (litevar_status s = strides_of(kv_strides, B, H_kv, kv_len, D, a.ks)) return s;
+  if (litevar_status s = strides_of(o_strides, B, H, q_len, D, a.os)) return s;
+  if (q_len == 0) return LITEVAR_OK;
+  if (!a.q || !a.o || (kv_len > 0 && (!a.k || !a.v))) return fail(LITEVAR_E_INVALID_ARG, "q, k, v or o is NULL");
+  if (a.o == a.q || (kv_len > 0 && (a.o == a.k || a.o == a.v))) return fail(LITEVAR_E_INVALID_ARG, "o aliases an input");
+  if (((uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v | (uintptr_t)a.o) & 15)
+    return fail(LITEVAR_E_INVALID_ARG, "q, k, v, o must be 16-byte aligned");
+  if ((uintptr_t)a.len & 3) return fail(LITEVAR_E_INVALID_ARG, "lengths must be 4-byte aligned");
+  size_t need = 0;
+  if (litevar_status s = litevar_cross_attn_workspace_bytes(B, H, H_kv, q_len, kv_len, &need)) return s;
+  if (need > 0 && !d_workspace) return fail(LITEVAR_E_INVALID_ARG, "d_workspace is NULL");
+  if (workspace_bytes < need) return fail(LITEVAR_E_INVALID_ARG, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+  if (need > 0 && ((uintptr_t)d_workspace & 15)) return fail(LITEVAR_E_INVALID_ARG, "d_workspace must be 16-byte aligned");
+  a.B = B; a.H = H; a.Hkv = H_kv; a.G = H / H_kv; a.q_len = q_len; a.kv_len = kv_len;
+  a.rows = a.G * q_len; a.tiles = (a.rows + kRows - 1) / kRows;
+  const int64_t tiles = tiles_of(B, H, H_kv, q_len);
+  a.parts = parts_of(tiles, kv_len);
+  a.scale_blocks = (kv_len + kBlock - 1) / kBlock;
+  a.q_magic = magic_of(q_len); a.tiles_magic = magic_of(a.tiles); a.hkv_magic = magic_of(H_kv); a.parts_magic = magic_of(a.parts);
+  a.part_o = (float*)d_workspace;
+  a.part_ml = (float2*)((char*)d_workspace + (size_t)tiles * a.parts * kRows * 64 * 4);
+  const float c = sm_scale * 1.4426950408889634f;
+  hipStream_t st = (hipStream_t)stream;
+  if (kind == kF32) return launch<kF32>(a, c, st);
+  if (kind == kCodes) return launch<kCodes>(a, c, st);
+  return launch<kBf16>(a, c, st);
+}
+
+}  // namespace
+}  // namespace lv
+
+using namespace lv;
+
+extern "C" {
+
+litevar_status litevar_cross_attn_workspace_bytes(int32_t B, int32_t H, int32_t H_kv, int32_t q_len, int32_t kv_len,
+                                                  size_t* out_bytes) {
+  if (!out_bytes) return fail(LITEVAR_E_INVALID_ARG, "out_bytes is NULL");
+  if (litevar_status s = check_shape(B, H, H_kv, q_len, kv_len)) return s;
+  const int64_t tiles = tiles_of(B, H, H_kv, q_len), parts = parts_of(tiles, kv_len);
+  *out_bytes = parts > 1 ? (size_t)tiles * parts * kRows * (64 * 4 + 8) : 0;
+  return LITEVAR_OK;
+}
+
+litevar_status litevar_cross_attn_fwd(const void* d_q, const void* d_k, const void* d_v, void* d_o, int32_t B, int32_t H,
+                                      int32_t H_kv, int32_t q_len, int32_t kv_len, int32_t D, litevar_dtype dt,
+                                      const int64_t* q_strides, const int64_t* kv_strides, const int64_t* o_strides,
+                                      const int32_t* d_kv_len, float sm_scale, void* d_workspace, size_t workspace_bytes,
+                                      void* stream) {
+  if (dt != LITEVAR_BF16 && dt != LITEVAR_F32) return fail(LITEVAR_E_UNSUPPORTED, "unknown dtype %d", (int)dt);
+  CrossArgs a{};
+  a.q = d_q; a.k = d_k; a.v = d_v; a.o = d_o; a.len = d_kv_len;
+  return cross_attention(a, dt == LITEVAR_F32 ? kF32 : kBf16, B, H, H_kv, q_len, kv_len, D, q_strides, kv_strides, o_strides,
+                         sm_scale, d_workspace, workspace_bytes, stream);
+}
+
+litevar_status litevar_cross_attn_kv8_fwd(const void* d_q, const int8_t* d_k8, const float* d_k_scale, const int8_t* d_v8,
+                                          const float* d_v_scale, void* d_o, int32_t B, int32_t H, int32_t H_kv, int32_t q_len,
+                                          int32_t kv_len, int32_t D, const int64_t* q_strides, const int64_t* o_strides,
+                                          const int32_t* d_kv_len, float sm_scale, void* d_workspace, size_t workspace_bytes,
+                                          void* stream) {
+  if (kv_len > 0 && (!d_k_scale || !d_v_scale)) return fail(LITEVAR_E_INVALID_ARG, "a scale pointer is NULL");
+  if (((uintptr_t)d_k_scale | (uintptr_t)d_v_scale) & 3) return fail(LITEVAR_E_INVALID_ARG, "scales must be 4-byte aligned");
+  CrossArgs a{};
+  a.q = d_q; a.k = d_k8; a.v = d_v8; a.o = d_o; a.len = d_kv_len; a.k_scale = d_k_scale; a.v_scale = d_v_scale;
+  return cross_attention(a, kCodes, B, H, H_kv, q_len, kv_len, D, q_strides, nullptr, o_strides, sm_scale, d_workspace,
+                         workspace_bytes, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,159 @@
+"""Windowed attention on the 8-bit cache against the formula in 64 bits on the cache's own values.
+
+Tolerance, element by element (A = sum of weights x |v|, S = the row's largest sum of |q_d k_d| x sm_scale, U = half a
+step of bf16): V rounded, U A; probabilities rounded, 2 U A; output rounded, U A; K rounded, which moves a score by
+U S at most and so a weight by the factor exp(2 U S): (exp(2 U S) - 1) 2 A.  Sums in 32 bits: below U A / 8."""
+import pytest
+import torch
+
+import _kv8_plain as plain
+import workloads
+
+pytestmark = pytest.mark.gpu
+SM = 0.125
+VAR256 = workloads.configs.VAR256
+
+
+@pytest.fixture(scope="module")
+def lv():
+    import paper_2411_17178_amd as m
+    m.load_library()
+    return m
+
+
+def _tolerance(A, S):
+    return (4.125 * plain.U + 2 * torch.expm1(2 * plain.U * S)) * A
+
+
+def _cache(lv, scales, B, H, seed, seen=None):
+    """A cache with the scales before `seen` stored (default: all), nothing usable behind them."""
+    seg = [s * s for s in scales]
+    seen = len(seg) if seen is None else seen
+    cache = lv.litevar_kv8_cache(seg, B, H)
+    for t in (cache.k_scale, cache.v_scale):
+        t.fill_(float("nan"))
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    n = cache.offsets[seen]
+    k, v = (torch.randn(B, H, n, 64, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    lv.litevar_kv8_store(cache, k, v, (0, seen))
+    return cache
+
+
+def _reference(cache, q, mask, sm=SM):
+    kd, vd = (plain.dequantise(c, s, cache.segments) for c, s in ((cache.k8, cache.k_scale), (cache.v8, cache.v_scale)))
+    used = mask.any(-2 if mask.dim() == 2 else 1)                            # tokens that some query keeps
+    used = used.view(1, -1, mask.shape[-1], 1)
+    zero = torch.zeros((), dtype=torch.float64, device="cuda")
+    return plain.attention(q, torch.where(used, kd, zero), torch.where(used, vd, zero), mask, sm)
+
+
+CASES = [  # scales, query scales, radius, sink scales, mask mode, batch, heads, plan options
+    ((1, 2, 3, 4), None, 1, 0, 0, 1, 1, 0), (VAR256, (0, 1), 3, 0, 0, 2, 3, 0), (VAR256, (3, 4), 2, 0, 0, 2, 16, 0),
+    (VAR256, (6, 7), 3, 0, 0, 2, 5, 0), (VAR256, (7, 8), 3, 3, 0, 3, 5, 0), (VAR256, (9, 10), 3, 0, 0, 4, 30, 0),
+    (VAR256, (9, 10), 3, 0, 0, 4, 30, 16), (VAR256, (9, 10), 3, 0, 0, 2, 3, (16, 0, 0, -1, 1)),
+    (VAR256, None, 2, 0, 0, 2, 16, 0), (VAR256, None, 2, 0, 0, 2, 16, 16), (VAR256, None, -1, 0, 0, 2, 30, 0),
+    (VAR256, (9, 10), -1, 0, 0, 2, 30, 0), (VAR256, None, 12, 0, 1, 2, 4, 0), (VAR256, (8, 9), 24, 0, 1, 2, 4, 16),
+    ((5, 9, 7, 13), None, 2, 0, 0, 2, 3, 16), ((5, 9, 7, 13), (2, 3), 2, 1, 0, 2, 3, 8), ((1,) * 20 + (12,), (20, 21), 1, 0, 0, 1, 2, 16),
+    (workloads.configs.VAR512, None, 4, 0, 0, 2, 6, 0), (workloads.configs.VAR512, (9, 10), 4, 0, 0, 2, 36, 0),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: f"{len(c[0])}x{c[0][-1]}-{c[1]}-r{c[2]}-s{c[3]}-m{c[4]}-{c[5]}x{c[6]}-{c[7]}")
+def test_windowed_attention_on_the_cache(lv, case):
+    scales, q_scales, radius, sink, mode, B, H, waves = case
+    print(f"  windowed kv8 {case}", flush=True)
+    plan = lv.litevar_mask_build(scales, radius, None, sink, q_scales, waves_per_group=waves, mask_mode=mode)
+    cache = _cache(lv, scales, B, H, 1, None if q_scales is None else q_scales[1])
+    g = torch.Generator(device="cuda").manual_seed(2)
+    q = torch.randn(B, H, plan.q_len, 64, generator=g, device="cuda").to(torch.bfloat16)
+    out = lv.litevar_windowed_attn_kv8_fwd(plan, q, cache, SM)
+    mask = lv.litevar_mask_export_dense(plan)[0].bool()
+    want, A, S = _reference(cache, q, mask)
+    plain.assert_close(out, want, _tolerance(A, S))
+    lv.litevar_plan_check(plan)
+
+
+def test_one_radius_table_per_head(lv):
+    K, H, B = len(VAR256), 4, 2
+    tables = [[[(h + j) % 4 for j in range(K)] for _ in range(K)] for h in range(H)]
+    for waves, q_scales in ((0, (9, 10)), (16, None), (4, (5, 6))):
+        plan = lv.litevar_mask_build(VAR256, 0, tables, 0, q_scales, waves_per_group=waves)
+        cache = _cache(lv, VAR256, B, H, 3, None if q_scales is None else q_scales[1])
+        q = torch.randn(B, H, plan.q_len, 64, device="cuda").to(torch.bfloat16)
+        out = lv.litevar_windowed_attn_kv8_fwd(plan, q, cache, SM)
+        mask = torch.stack([lv.litevar_mask_export_dense(plan, head=h)[0].bool() for h in range(H)])
+        want, A, S = _reference(cache, q, mask)
+        plain.assert_close(out, want, _tolerance(A, S))
+
+
+@pytest.mark.parametrize("waves", [0, 16])
+def test_output_sharing_and_strides(lv, waves):
+    B, H = 4, 6
+    plan = lv.litevar_mask_build(VAR256, 3, None, 0, (9, 10), waves_per_group=waves)
+    cache = _cache(lv, VAR256, B, H, 4)
+    share = (torch.arange(H)[:, None] % 2 == 0).expand(H, 10).contiguous().to(torch.uint8).cuda()
+    q = torch.randn(B, 256, H, 64, device="cuda").to(torch.bfloat16).transpose(1, 2)
+    big = torch.full((B, 258, H, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = big[:, 1:-1].transpose(1, 2)
+    lv.litevar_windowed_attn_kv8_fwd(plan, q, cache, SM, out=out, cfg_share=share)
+    alone = lv.litevar_windowed_attn_kv8_fwd(plan, q, cache, SM)
+    shared = share[:, 9].bool()
+    assert torch.equal(out[:2], alone[:2]) and torch.equal(out[2:, ~shared], alone[2:, ~shared])
+    assert torch.equal(out[2:, shared], out[:2, shared])
+    assert bool((big[:, 0] == 7).all()) and bool((big[:, -1] == 7).all())
+
+
+def test_values_that_are_not_finite_stay_in_their_rows(lv):
+    """A block whose scale is not finite reaches the queries that keep one of its tokens and no others."""
+    B, H = 1, 2
+    for waves in (16,):
+        plan = lv.litevar_mask_build(VAR256, 1, None, 0, None, waves_per_group=waves)
+        cache = _cache(lv, VAR256, B, H, 5)
+        block = cache.first_block[9] + 1                                     # tokens 64 .. 127 of the last scale
+        cache.v_scale[0, 1, block] = float("inf")
+        q = torch.randn(B, H, plan.q_len, 64, device="cuda").to(torch.bfloat16)
+        out = lv.litevar_windowed_attn_kv8_fwd(plan, q, cache, SM)
+        mask = lv.litevar_mask_export_dense(plan)[0].bool()
+        lo = cache.offsets[9] + 64
+        hit = mask[:, lo:lo + 64].any(-1)
+        clean = _cache(lv, VAR256, B, H, 5)
+        want, A, S = _reference(clean, q, mask)
+        tol = _tolerance(A, S)
+        plain.assert_close(out[:, :1], want[:, :1], tol[:, :1])
+        plain.assert_close(out[:, 1, ~hit], want[:, 1, ~hit], tol[:, 1, ~hit])
+        assert not bool(torch.isfinite(out[:, 1, hit]).all(-1).any())
+
+
+def test_whole_generation_with_graph(lv):
+    """All steps of a layer, one captured graph each: the scale is stored, then attended to."""
+    B, H = 2, 6
+    seg = [s * s for s in VAR256]
+    plans = [lv.litevar_mask_build(VAR256, 3, None, 0, (k, k + 1)) for k in range(10)]
+    full = lv.litevar_mask_build(VAR256, 3)
+    mask = lv.litevar_mask_export_dense(full)[0].bool()
+    cache = lv.litevar_kv8_cache(seg, B, H)
+    q, k, v = (torch.randn(B, H, 680, 64, device="cuda").to(torch.bfloat16) for _ in range(3))
+    work = torch.empty(max(lv.litevar_windowed_attn_kv8_workspace_bytes(p, B, H) for p in plans), dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(q)
+
+    def steps():
+        for i, p in enumerate(plans):
+            lo, hi = cache.offsets[i], cache.offsets[i + 1]
+            lv.litevar_kv8_store(cache, k[:, :, lo:hi], v[:, :, lo:hi], (i, i + 1))
+            lv.litevar_windowed_attn_kv8_fwd(p, q[:, :, lo:hi], cache, SM, out=out[:, :, lo:hi], workspace=work)
+    steps()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        steps()
+    for i in range(3):
+        q.copy_(torch.randn(q.shape, device="cuda"))
+        k.copy_(torch.randn(q.shape, device="cuda"))
+        cache.k8.zero_()
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        want, A, S = _reference(cache, q, mask)
+        plain.assert_close(out, want, _tolerance(A, S))
+        replayed = out.clone()
+        steps()
+        assert torch.equal(out, replayed)
