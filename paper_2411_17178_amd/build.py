@@ -11,7 +11,8 @@ LIB = os.path.join(HERE, "liblitevar.so")
 TABLES = os.path.join(HERE, "_tables" + sysconfig.get_config_var("EXT_SUFFIX"))   # the Python binding's own module
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "plan_build.hip", "attn_f32.hip", "attn_bf16.hip", "attn_bf16_pair.hip", "attn_bf16_dense.hip",
-           "calibrate.hip", "calibrate_band.hip", "peaks.hip", "qkv8.hip", "kv8.hip", "attn_cross.hip"]
+           "calibrate.hip", "calibrate_band.hip", "peaks.hip", "qkv8.hip", "kv8.hip", "attn_kv8.hip",
+           "attn_cross.hip"]
 # -fno-honor-nans: the kernels never produce NaN from finite inputs (masked scores are -inf
 # and the softmax reference starts at a finite floor), and it spares the canonicalising
 # v_max that IEEE maxNum semantics would need in front of every fmaxf.

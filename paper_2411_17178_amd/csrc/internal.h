@@ -106,6 +106,15 @@ int64_t spread_over_xcds(AttnArgs& a, int64_t items, int row_bytes);
 litevar_status make_attn_args(const litevar_plan* plan, int32_t B, int32_t H, int32_t D, float sm_scale,
                               const uint8_t* d_cfg_share, uint32_t flags, AttnArgs& a);
 
+// The block scales of an 8-bit cache whose segments are a plan's scales: token t of segment j lies in block
+// (t + shift[j]) / 64, segment j begins at token off[j].
+struct KV8Scales {
+  const float* k; const float* v;              // [B][H][n_blocks]
+  int n_blocks;
+  int off[kMaxScales + 1], shift[kMaxScales + 1];
+};
+
+litevar_status launch_attn_kv8(const litevar_plan* pl, const AttnArgs& a, const KV8Scales& scales, hipStream_t st);
 litevar_status launch_attn_f32(const litevar_plan* pl, const AttnArgs& a, hipStream_t st);
 litevar_status launch_attn_bf16(const litevar_plan* pl, const AttnArgs& a, hipStream_t st);
 litevar_status launch_attn_bf16_pair(const litevar_plan* pl, const AttnArgs& a, hipStream_t st);

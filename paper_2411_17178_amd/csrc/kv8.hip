@@ -204,11 +204,6 @@ litevar_status launch_blocks(Blocks& w, const char* what, Launch launch) {
   });
 }
 
-// the segments of a plan's cache: its scales
-void plan_segments(const litevar_plan* plan, int32_t (&seg)[kMaxScales]) {
-  for (int k = 0; k < plan->n_scales; ++k) seg[k] = plan->scales[k] * plan->scales[k];
-}
-
 // (the stride of an axis with one entry is never used, and is what it is)
 litevar_status check_rows(const int64_t* s, int B, int H, int64_t n, int D, int64_t (&out)[3]) {
   if (!s) { out[2] = D; out[1] = n * D; out[0] = (int64_t)H * n * D; return LITEVAR_OK; }
@@ -278,7 +273,7 @@ litevar_status litevar_kv8_load(const int32_t* segments, int32_t n_segments, int
 litevar_status litevar_windowed_attn_kv8_workspace_bytes(const litevar_plan* plan, int32_t B, int32_t H, size_t* out_bytes) {
   if (!plan || !out_bytes) return fail(LITEVAR_E_INVALID_ARG, "plan or out_bytes is NULL");
   if (B < 1 || H < 1) return fail(LITEVAR_E_INVALID_ARG, "B and H must be positive");
-  *out_bytes = (size_t)B * H * 2 * (size_t)plan->kv_len * 64 * 2;
+  *out_bytes = 0;
   return LITEVAR_OK;
 }
 
@@ -288,32 +283,31 @@ litevar_status litevar_windowed_attn_kv8_fwd(const litevar_plan* plan, const voi
                                              const uint8_t* d_cfg_share, uint32_t flags, void* d_workspace,
                                              size_t workspace_bytes, void* stream) {
   if (!d_q || !d_k8 || !d_k_scale || !d_v8 || !d_v_scale || !d_o) return fail(LITEVAR_E_INVALID_ARG, "a pointer is NULL");
-  AttnArgs check;
-  if (litevar_status s = make_attn_args(plan, B, H, D, sm_scale, d_cfg_share, flags, check)) return s;
+  AttnArgs a;
+  if (litevar_status s = make_attn_args(plan, B, H, D, sm_scale, d_cfg_share, flags, a)) return s;
   size_t need = 0;
   if (litevar_status s = litevar_windowed_attn_kv8_workspace_bytes(plan, B, H, &need)) return s;
-  if (!d_workspace) return fail(LITEVAR_E_INVALID_ARG, "d_workspace is NULL");
+  if (need > 0 && !d_workspace) return fail(LITEVAR_E_INVALID_ARG, "d_workspace is NULL");
   if (workspace_bytes < need) return fail(LITEVAR_E_INVALID_ARG, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
-  if ((uintptr_t)d_workspace & 255) return fail(LITEVAR_E_INVALID_ARG, "d_workspace must be 256-byte aligned");
-  // (everything that the attention call below would refuse, before the first launch)
-  int64_t qs[3], os[3];
-  if (litevar_status s = check_rows(q_strides, B, H, plan->q_len, D, qs)) return s;
-  if (litevar_status s = check_rows(o_strides, B, H, plan->q_len, D, os)) return s;
-  if (d_o == d_q || d_o == d_workspace) return fail(LITEVAR_E_INVALID_ARG, "o aliases an input");
+  if (need > 0 && ((uintptr_t)d_workspace & 255)) return fail(LITEVAR_E_INVALID_ARG, "d_workspace must be 256-byte aligned");
+  if (litevar_status s = check_rows(q_strides, B, H, plan->q_len, D, a.qs)) return s;
+  if (litevar_status s = check_rows(o_strides, B, H, plan->q_len, D, a.os)) return s;
+  if (d_o == d_q) return fail(LITEVAR_E_INVALID_ARG, "o aliases an input");
   if (((uintptr_t)d_q | (uintptr_t)d_k8 | (uintptr_t)d_v8 | (uintptr_t)d_o) & 15)
     return fail(LITEVAR_E_INVALID_ARG, "q, o and the codes must be 16-byte aligned");
   if (((uintptr_t)d_k_scale | (uintptr_t)d_v_scale) & 3) return fail(LITEVAR_E_INVALID_ARG, "scales must be 4-byte aligned");
-  if ((int64_t)plan->kv_len * 128 >= ((int64_t)1 << 31))
-    return fail(LITEVAR_E_UNSUPPORTED, "one (batch, head) slab of k/v spans 2 GiB or more");
-  // Only the scales that the queries see are copied; the attention kernels read no other rows.
-  int32_t seg[kMaxScales];
-  plan_segments(plan, seg);
-  __bf16* k = (__bf16*)d_workspace;
-  __bf16* v = k + (int64_t)B * H * plan->kv_len * 64;
-  if (litevar_status s = litevar_kv8_load(seg, plan->n_scales, 0, plan->q_scale_end, d_k8, d_k_scale, d_v8, d_v_scale, B, H, D,
-                                          k, v, stream)) return s;
-  return litevar_windowed_attn_fwd(plan, d_q, k, v, d_o, B, H, D, LITEVAR_BF16, qs, nullptr, os, sm_scale,
-                                   d_cfg_share, flags, stream);
+  a.q = d_q; a.k = d_k8; a.v = d_v8; a.o = d_o;
+  a.ks[2] = 64; a.ks[1] = (int64_t)plan->kv_len * 64; a.ks[0] = a.ks[1] * H;
+  KV8Scales scales{};
+  scales.k = d_k_scale; scales.v = d_v_scale;
+  int off = 0, first = 0;
+  for (int k = 0; k <= kMaxScales; ++k) {
+    scales.off[k] = off; scales.shift[k] = kBlock * first - off;
+    const int n = k < plan->n_scales ? plan->scales[k] * plan->scales[k] : 0;
+    off += n; first += (n + kBlock - 1) / kBlock;
+  }
+  scales.n_blocks = first;
+  return launch_attn_kv8(plan, a, scales, (hipStream_t)stream);
 }
 
 }  // extern "C"
