@@ -316,4 +316,32 @@ template <int NW> __device__ inline int lds_min_progress(const int32_t* p) {
   return min(m0, m1);
 }
 
+// ---- K and V rows of 128 bytes in LDS, in blocks of 32 keys (the kernels that walk keys in token order) ----
+constexpr int kRow = 128;                      // bytes of a K or V row
+
+// 16-byte piece p of row r is stored at piece position p ^ swizzle(r): eight consecutive rows put
+// one piece into eight places (K reads), and four consecutive rows put a 32-byte unit into the four
+// units of the row (the transposing V reads: 4 keys x 32 bytes per 16 lanes).
+__device__ inline unsigned dense_swizzle(unsigned r) { return ((r & 3u) << 1) | ((r >> 2) & 1u); }
+
+// K rows of a block as the A operand and its V rows, transposed: va[4 t + 2 j + dt], slice t of 16 keys, its half j, head
+// dimension tile dt.  Issued only; a wait must precede the first use.  AT: byte offset of the block's rows.
+template <int AT>
+__device__ inline void read_k(const unsigned (&k)[4], u32x4 (&r)[4]) {
+  asm volatile("ds_read_b128 %0, %4 offset:%8\n\tds_read_b128 %1, %5 offset:%8\n\t"
+               "ds_read_b128 %2, %6 offset:%8\n\tds_read_b128 %3, %7 offset:%8"
+               : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3])
+               : "v"(k[0]), "v"(k[1]), "v"(k[2]), "v"(k[3]), "i"(AT) : "memory");
+}
+template <int AT>
+__device__ inline void read_v(const unsigned (&v)[2], u32x2 (&va)[8]) {
+  asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%10\n\tds_read_b64_tr_b16 %1, %9 offset:%10\n\t"
+               "ds_read_b64_tr_b16 %2, %8 offset:%11\n\tds_read_b64_tr_b16 %3, %9 offset:%11\n\t"
+               "ds_read_b64_tr_b16 %4, %8 offset:%12\n\tds_read_b64_tr_b16 %5, %9 offset:%12\n\t"
+               "ds_read_b64_tr_b16 %6, %8 offset:%13\n\tds_read_b64_tr_b16 %7, %9 offset:%13"
+               : "=&v"(va[0]), "=&v"(va[1]), "=&v"(va[2]), "=&v"(va[3]),
+                 "=&v"(va[4]), "=&v"(va[5]), "=&v"(va[6]), "=&v"(va[7])
+               : "v"(v[0]), "v"(v[1]), "i"(AT), "i"(AT + 8 * kRow), "i"(AT + 16 * kRow), "i"(AT + 24 * kRow) : "memory");
+}
+
 }  // namespace lv

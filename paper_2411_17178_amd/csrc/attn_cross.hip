@@ -7,6 +7,7 @@
 // blocks of 64 keys (32 in fp32) in turn and join their results through LDS.  With several parts, each leaves its sums
 // in the workspace and a second launch joins them.
 #include <cstring>
+#include <type_traits>
 
 #include "attn_bf16_common.h"
 
@@ -29,7 +30,7 @@ struct CrossArgs {
   int rows, tiles;                             // rows of a kv head, tiles of 32 of them
   int parts;                                   // of the key axis
   int scale_blocks;                            // of a (batch, kv head)
-  uint32_t q_magic, tiles_magic, hkv_magic, parts_magic;   // see divmod_by
+  uint32_t q_magic, tiles_magic, hkv_magic, parts_magic, pairs_magic;   // see divmod_by
   uint32_t first_block;
   float* part_o; float2* part_ml;              // [item][32][64] and [item][32] (largest score, sum), item = workgroup
 };
@@ -43,8 +44,6 @@ __device__ inline Row row_at(const CrossArgs& a, int j, int r) {
 }
 
 __device__ inline int keys_of(const CrossArgs& a, int b) { return a.len ? min(max(a.len[b], 0), a.kv_len) : a.kv_len; }
-
-__device__ inline unsigned swizzle(unsigned r) { return ((r & 3u) << 1) | ((r >> 2) & 1u); }
 
 // eight codes (a word pair) as bf16, exactly
 __device__ inline bf16x8 codes_to_bf16(unsigned lo, unsigned hi) {
@@ -202,8 +201,8 @@ __global__ __launch_bounds__(kWaves * 64) void k_cross_rows(CrossArgs a, float c
             const int row = 16 * i + (lane >> 2), key = key0 + row, p = 2 * (lane & 3);
             const u32x4 x = *(const u32x4*)((const int8_t*)a.v + kv_at + (int64_t)min(key, n_keys - 1) * a.ks[2] + 8 * p);
             const bf16x8 lo = codes_to_bf16(x[0], x[1]), hi = codes_to_bf16(x[2], x[3]);
-            *(bf16x8*)(Vs + row * 128 + (((unsigned)p ^ swizzle((unsigned)row)) << 4)) = lo;
-            *(bf16x8*)(Vs + row * 128 + (((unsigned)(p + 1) ^ swizzle((unsigned)row)) << 4)) = hi;
+            *(bf16x8*)(Vs + row * 128 + (((unsigned)p ^ dense_swizzle((unsigned)row)) << 4)) = lo;
+            *(bf16x8*)(Vs + row * 128 + (((unsigned)(p + 1) ^ dense_swizzle((unsigned)row)) << 4)) = hi;
           }
         } else {
           const __bf16* kp = (const __bf16*)a.k + kv_at + k_row + 32 * hh;
@@ -216,7 +215,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_cross_rows(CrossArgs a, float c
           for (int i = 0; i < 4; ++i) {
             const int row = 8 * i + (lane >> 3);
             const uint4 x = *(const uint4*)((const __bf16*)a.v + kv_at + (int64_t)min(key0 + row, n_keys - 1) * a.ks[2] + 8 * (lane & 7));
-            *(uint4*)(Vs + row * 128 + ((((unsigned)lane & 7u) ^ swizzle((unsigned)row)) << 4)) = x;
+            *(uint4*)(Vs + row * 128 + ((((unsigned)lane & 7u) ^ dense_swizzle((unsigned)row)) << 4)) = x;
           }
         }
         softmax(S, key0);
@@ -242,7 +241,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_cross_rows(CrossArgs a, float c
             for (int jj = 0; jj < 2; ++jj) {
               const unsigned l16 = (unsigned)lane & 15u, row = 16u * t + 8u * jj + 4u * (unsigned)hh + (l16 >> 2);
               const unsigned piece = 4u * dt + 2u * (((unsigned)lane >> 4) & 1u) + ((l16 & 3u) >> 1);
-              const s16x4 x = lds_read_tr16(Vs + row * 128 + ((piece ^ swizzle(row)) << 4) + 8u * (l16 & 1u));
+              const s16x4 x = lds_read_tr16(Vs + row * 128 + ((piece ^ dense_swizzle(row)) << 4) + 8u * (l16 & 1u));
 #pragma unroll
               for (int e = 0; e < 4; ++e) v8[4 * jj + e] = x[e];
             }
@@ -287,6 +286,291 @@ __global__ __launch_bounds__(kWaves * 64) void k_cross_rows(CrossArgs a, float c
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] *= inv;
   store_row<KIND>(a, b, j, row0 + row, dims, x);
+}
+
+// Many rows: NWV waves of one (batch, kv head), each with 32 rows, share the K and V rows, which pass through LDS in chunks
+// of 64 keys, three buffers: one read, one landing, one whose last readers may be behind, so that one barrier per chunk
+// is enough.  bf16 rows come by LDS-DMA; codes through registers, converted (exactly) on their way, one chunk ahead.  The
+// score products of a block of 32 keys are issued ahead of the exponentials of the block before it.
+//
+// Softmax in base 2: the reference is the largest score of the first block and moves when a sum passes 2^10, so that no
+// maximum is formed in the other blocks.  p = exp2(s c - m c) in one instruction where |m c| < 2^13 (beyond it the rounding
+// of m c would show; there the reference is subtracted before the scale is applied).
+//
+// Codes: a chunk is a block, its K scale joins the softmax scale.  Its V scale, relative to the largest of the
+// keys that count, is added to the exponent, which costs nothing per score; the chunk's part of the row sum is divided by it
+// again.  (Relative V scales are taken as at least 2^-96, so that no probability that counts is flushed to zero.)
+template <int NWV, int KIND>
+__global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(NWV == 4 ? 3 : 4, NWV == 4 ? 3 : 4)))
+void k_cross_tiles(CrossArgs a, float c) {
+  constexpr bool CODES = KIND == kCodes;
+  constexpr int kRowsPerWave = kBlock / NWV, kTransfers = kRowsPerWave / 8, kBuf = 2 * kBlock * kRow;
+  constexpr float kMost = 0x1p10f, kFar = 0x1p13f;
+  __shared__ __align__(1024) unsigned char smem[3 * kBuf];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int n = lane & 31, hh = lane >> 5;
+  // all (batch, kv head) pairs of one tile next to each other: workgroup i runs on XCD i % 8, so the tiles of a pair share
+  // an L2 where there are eight pairs to an eighth, and few pairs still use all XCDs
+  int tile, bj, b, j;
+  divmod_by(a.first_block + blockIdx.x, (uint32_t)(a.B * a.Hkv), a.pairs_magic, tile, bj);
+  divmod_by((uint32_t)bj, (uint32_t)a.Hkv, a.hkv_magic, b, j);
+  const int n_keys = keys_of(a, b);
+  const int row0 = (tile * NWV + wave) * kRows;
+  const bool working = row0 < a.rows;          // (uniform)
+  const Row qr = row_at(a, j, min(row0 + n, a.rows - 1));    // (a column without a row holds the last one; it is not stored)
+  bf16x8 qf[4];
+  {
+    const __bf16* qp = (const __bf16*)a.q + b * a.qs[0] + qr.h * a.qs[1] + qr.i * a.qs[2] + 8 * hh;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) qf[t] = as_bf16x8(*(const uint4*)(qp + 16 * t));
+  }
+  const int n_chunks = (n_keys + kBlock - 1) / kBlock;
+  __builtin_amdgcn_sched_barrier(0);           // (the loads of Q stay ahead of the transfers, which are counted below)
+
+  // ---- loading duty ----
+  const int64_t kv_at = b * a.ks[0] + j * a.ks[1];
+  const int lrow = lane >> 3;
+  const unsigned piece_off = (((unsigned)lane & 7u) ^ dense_swizzle((unsigned)lrow)) << 4;
+  [[maybe_unused]] auto issue_chunk = [&](int chunk, int buf) {
+#pragma unroll
+    for (int i = 0; i < kTransfers; ++i) {
+      const int r0 = kRowsPerWave * wave + 8 * i, key = min(kBlock * chunk + r0 + lrow, n_keys - 1);
+      const int64_t src = (kv_at + key * a.ks[2]) * 2 + piece_off;
+      unsigned char* dst = smem + buf * kBuf + r0 * kRow;
+      __builtin_amdgcn_global_load_lds((global_void*)((const unsigned char*)a.k + src), (lds_void*)dst, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((global_void*)((const unsigned char*)a.v + src), (lds_void*)(dst + kBlock * kRow), 16, 0, 0);
+    }
+  };
+  // codes: 16 of a K or V row per thread and piece, 512 pieces to a chunk
+  constexpr int kPieces = 512 / (NWV * 64);
+  [[maybe_unused]] u32x4 codes[kPieces];
+  [[maybe_unused]] auto load_chunk = [&](int chunk) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int at = tid + NWV * 64 * i, key = min(kBlock * chunk + ((at & 255) >> 2), n_keys - 1);
+      codes[i] = *(const u32x4*)((const int8_t*)(at < 256 ? a.k : a.v) + kv_at + (int64_t)key * 64 + 16 * (at & 3));
+    }
+  };
+  [[maybe_unused]] auto commit_chunk = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int at = tid + NWV * 64 * i, row = (at & 255) >> 2;
+      const unsigned p = 2u * ((unsigned)at & 3u), sw = dense_swizzle((unsigned)row);
+      unsigned char* dst = smem + buf * kBuf + (at < 256 ? 0 : kBlock * kRow) + row * kRow;
+      *(bf16x8*)(dst + ((p ^ sw) << 4)) = codes_to_bf16(codes[i][0], codes[i][1]);
+      *(bf16x8*)(dst + (((p + 1u) ^ sw) << 4)) = codes_to_bf16(codes[i][2], codes[i][3]);
+    }
+  };
+  // scales of 64 chunks at a time, lane i chunk i's: K's, log2 of V's over the largest, and its inverse
+  [[maybe_unused]] float vmax = 0.f, my_ks = 1.f, my_lv = 0.f, my_iv = 1.f;
+  [[maybe_unused]] auto load_scales = [&](int chunk) {
+    const int64_t at = (int64_t)bj * a.scale_blocks + min(chunk + lane, n_chunks - 1);
+    my_ks = a.k_scale[at];
+    const float vs = a.v_scale[at], rel = vs > 0.f && vmax > 0.f ? fmaxf(vs / vmax, 0x1p-96f) : 1.f;
+    my_lv = __builtin_amdgcn_logf(rel); my_iv = 1.f / rel;         // (base 2)
+  };
+
+  // LDS read offsets: K piece 2 t + hh of row n; V: 4 keys x 16 dims per 16 lanes
+  unsigned k_off[4], v_off[2];
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+    k_off[t] = lds_addr(smem) + (unsigned)n * kRow + ((((unsigned)(2 * t + hh)) ^ dense_swizzle((unsigned)n)) << 4);
+#pragma unroll
+  for (int dt = 0; dt < 2; ++dt) {
+    const unsigned l16 = (unsigned)lane & 15u, r = 4u * (unsigned)hh + (l16 >> 2);
+    const unsigned piece = 4u * dt + 2u * (((unsigned)lane >> 4) & 1u) + ((l16 & 3u) >> 1);
+    v_off[dt] = lds_addr(smem) + r * kRow + ((piece ^ dense_swizzle(r)) << 4) + 8u * (l16 & 1u);
+  }
+
+  f32x16 O[2] = {f32x16{}, f32x16{}};
+  float L[2] = {0.f, 0.f}, m = 0.f, negm = 0.f;          // this lane's part of the row sum; the reference, and minus it in base 2
+  bool unset = true;
+  uint64_t far = 0;
+
+  auto scores = [&](u32x4 (&kr)[4]) -> f32x16 {
+    lds_wait_k(kr[0], kr[1], kr[2], kr[3]);
+    f32x16 S = f32x16{};
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[t]), qf[t], S, 0, 0, 0);
+    return S;
+  };
+  // the rest of a block, its V rows requested; ks, lv, iv: of its chunk
+  auto absorb = [&](f32x16& S, u32x2 (&va)[8], int key0, float ks, float lv, float iv) {
+    if (key0 + 32 > n_keys) {                  // (uniform)
+      const int left = n_keys - key0 - 4 * hh;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) S[e] = 8 * (e >> 2) + (e & 3) < left ? S[e] : -INFINITY;
+    }
+    auto largest = [&]() {                     // score of the row, over both of its lanes
+      float mx = S[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, S[e]);
+      return fmaxf(mx, other_half(mx)) * ks;
+    };
+    auto set_reference = [&](float to) {
+      m = to; negm = -m * c;
+      far |= __builtin_amdgcn_ballot_w64(!(fabsf(negm) < kFar));
+    };
+    if (CODES && ks < 0x1p-100f) {             // (a block of zeros or nearly so: scaled here, c ks would lose its bits)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) S[e] = S[e] > -INFINITY ? S[e] * ks : S[e];
+      ks = 1.f;
+    }
+    if (unset) { set_reference(largest()); unset = false; }
+    bf16x8 pb[2];
+    float sum[2];
+    auto exponentials = [&]() {
+      const float cb = CODES ? c * ks : c, at = CODES ? negm + lv : negm;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        sum[t] = CODES ? 0.f : L[t];
+        if (__builtin_expect(far != 0, 0)) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float d = CODES ? __builtin_fmaf(S[8 * t + e], ks, -m) : S[8 * t + e] - m;
+            pb[t][e] = (__bf16)__builtin_amdgcn_exp2f(CODES ? __builtin_fmaf(d, c, lv) : d * c);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) pb[t][e] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(S[8 * t + e], cb, at));
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          const bf16x2 two = {pb[t][e], pb[t][e + 1]};
+          sum[t] = __builtin_amdgcn_fdot2_f32_bf16(two, kOnes, sum[t], false);
+        }
+        if constexpr (CODES) sum[t] = __builtin_fmaf(sum[t], iv, L[t]);
+      }
+    };
+    exponentials();
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(fmaxf(sum[0], sum[1]) > kMost) != 0, 0)) {
+      auto both = [&](const float (&x)[2]) { const float y = x[0] + x[1]; return y + other_half(y); };   // slices, lanes
+      const float now = both(sum), before = both(L);
+      float to = fmaxf(m, largest());
+      if (before > 1.f) to = fmaxf(to, m + __builtin_amdgcn_logf(before) / c);
+      to = now > kMost ? to : m;
+      const float alpha = __builtin_amdgcn_exp2f((m - to) * c);
+      set_reference(to);
+      L[0] *= alpha; L[1] *= alpha;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) { O[0][e] *= alpha; O[1][e] *= alpha; }
+      exponentials();
+    }
+    L[0] = sum[0]; L[1] = sum[1];
+    lds_wait_v_wide(va);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int dt = 0; dt < 2; ++dt) {
+        const uint4 v8 = {va[4 * t + dt].x, va[4 * t + dt].y, va[4 * t + 2 + dt].x, va[4 * t + 2 + dt].y};
+        O[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v8), pb[t], O[dt], 0, 0, 0);
+      }
+  };
+
+  if (n_chunks > 0) {
+    if constexpr (CODES) {
+      load_chunk(0);
+      for (int at = 0; at < n_chunks; at += 64) vmax = fmaxf(vmax, a.v_scale[(int64_t)bj * a.scale_blocks + min(at + lane, n_chunks - 1)]);
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) vmax = fmaxf(vmax, __shfl_xor(vmax, d));
+      commit_chunk(0);
+      if (n_chunks > 1) load_chunk(1);
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    } else {
+      issue_chunk(0, 0);
+      if (n_chunks > 1) { issue_chunk(1, 1); wait_vmcnt<2 * kTransfers>(); } else wait_vmcnt<0>();
+      asm volatile("" : "+v"(qf[0]), "+v"(qf[1]), "+v"(qf[2]), "+v"(qf[3]));   // (older than the chunks: in)
+      asm volatile("s_barrier" ::: "memory");
+    }
+    f32x16 S0 = f32x16{};                      // scores of the chunk's first block
+    if (working) {
+      u32x4 kr[4];
+      read_k<0>(k_off, kr);
+      S0 = scores(kr);
+    }
+    // A chunk: its two blocks, each with the next block's score products in front of its own exponentials.  Between the
+    // blocks the next chunk is made sure of and the one after it requested, for the buffer that every wave has read to
+    // its end by then.
+    auto one = [&](int chunk, auto which) -> bool {
+      constexpr int p = decltype(which)::value, AT = p * kBuf, NEXT = (p + 1) % 3 * kBuf;
+      const int key0 = chunk * kBlock;
+      const bool more = chunk + 1 < n_chunks, second = key0 + 32 < n_keys;
+      float ks = 1.f, lv = 0.f, iv = 1.f;
+      if constexpr (CODES) {
+        if ((chunk & 63) == 0) load_scales(chunk);
+        ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_ks), chunk & 63));
+        lv = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_lv), chunk & 63));
+        iv = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_iv), chunk & 63));
+      }
+      f32x16 S1;
+      asm volatile("" : "=v"(S1));             // (not set where there is no second block, and not used then)
+      if (working) {
+        u32x2 va[8];
+        if (second) {
+          u32x4 kr[4];
+          read_k<AT + 32 * kRow>(k_off, kr);
+          S1 = scores(kr);
+        }
+        read_v<AT + kBlock * kRow>(v_off, va);
+        __builtin_amdgcn_sched_barrier(0);
+        absorb(S0, va, key0, ks, lv, iv);
+      }
+      if (more) {
+        if constexpr (CODES) {
+          commit_chunk((p + 1) % 3);
+          if (chunk + 2 < n_chunks) load_chunk(chunk + 2);
+          asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        } else {
+          wait_vmcnt<0>();
+          asm volatile("s_barrier" ::: "memory");
+          if (chunk + 2 < n_chunks) issue_chunk(chunk + 2, (p + 2) % 3);
+        }
+      }
+      if (working && second) {
+        u32x2 va[8];
+        if (more) {
+          u32x4 kr[4];
+          read_k<NEXT>(k_off, kr);
+          S0 = scores(kr);
+        }
+        read_v<AT + (kBlock + 32) * kRow>(v_off, va);
+        __builtin_amdgcn_sched_barrier(0);
+        absorb(S1, va, key0 + 32, ks, lv, iv);
+      }
+      return more;
+    };
+    for (int chunk = 0;; chunk += 3) {
+      if (!one(chunk, std::integral_constant<int, 0>{})) break;
+      if (!one(chunk + 1, std::integral_constant<int, 1>{})) break;
+      if (!one(chunk + 2, std::integral_constant<int, 2>{})) break;
+    }
+  }
+
+  if (!working) return;
+  const float part = L[0] + L[1], l = part + other_half(part), inv = l > 0.f ? 1.f / l : 0.f, unit = CODES ? vmax : 1.f;   // (no key: zeros)
+  unsigned r[2][8];
+#pragma unroll
+  for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) {
+      float x = O[dt][e] * inv, y = O[dt][e + 1] * inv;
+      if constexpr (CODES) { x *= unit; y *= unit; }
+      r[dt][e / 2] = __builtin_bit_cast(unsigned, bf16x2{(__bf16)x, (__bf16)y});
+    }
+  if (row0 + n < a.rows) {
+    __bf16* op = (__bf16*)a.o + b * a.os[0] + qr.h * a.os[1] + qr.i * a.os[2] + 8 * hh;
+#pragma unroll
+    for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) {
+        // dims 32 dt + 16 jj .. + 15 of the row: its lanes hold 4 of each 8; exchanged, 8 in a row
+        const auto x0 = __builtin_amdgcn_permlane32_swap(r[dt][4 * jj], r[dt][4 * jj + 2], false, false);
+        const auto x1 = __builtin_amdgcn_permlane32_swap(r[dt][4 * jj + 1], r[dt][4 * jj + 3], false, false);
+        const u32x4 piece = {x0[0], x1[0], x0[1], x1[1]};
+        *(u32x4*)(op + 32 * dt + 16 * jj) = piece;
+      }
+  }
 }
 
 // Joins the parts of one tile of rows: a workgroup per (batch, kv head, tile).
@@ -347,6 +631,16 @@ litevar_status strides_of(const int64_t* s, int B, int heads, int64_t n, int D, 
 
 template <int KIND> litevar_status launch(CrossArgs& a, float c, hipStream_t st) {
   const int64_t tiles = (int64_t)a.B * a.Hkv * a.tiles;
+  if constexpr (KIND != kF32) {
+    if (a.parts == 1 && a.tiles > 1) {
+      const int nwv = a.tiles > 4 ? 8 : 4;
+      return launch_in_parts((int64_t)a.B * a.Hkv * ((a.tiles + nwv - 1) / nwv), nwv * 64, "cross attention launch", [&](int64_t first, unsigned n) {
+        a.first_block = (uint32_t)first;
+        if (nwv == 8) hipLaunchKernelGGL((k_cross_tiles<8, KIND>), dim3(n), dim3(512), 0, st, a, c);
+        else hipLaunchKernelGGL((k_cross_tiles<4, KIND>), dim3(n), dim3(256), 0, st, a, c);
+      });
+    }
+  }
   if (litevar_status s = launch_in_parts(tiles * a.parts, kWaves * 64, "cross attention launch", [&](int64_t first, unsigned n) {
         a.first_block = (uint32_t)first;
         hipLaunchKernelGGL(k_cross_rows<KIND>, dim3(n), dim3(kWaves * 64), 0, st, a, c);
@@ -388,6 +682,7 @@ litevar_status cross_attention(CrossArgs& a, Kind kind, int32_t B, int32_t H, in
   a.parts = parts_of(tiles, kv_len);
   a.scale_blocks = (kv_len + kBlock - 1) / kBlock;
   a.q_magic = magic_of(q_len); a.tiles_magic = magic_of(a.tiles); a.hkv_magic = magic_of(H_kv); a.parts_magic = magic_of(a.parts);
+  a.pairs_magic = magic_of((int64_t)B * H_kv);
   a.part_o = (float*)d_workspace;
   a.part_ml = (float2*)((char*)d_workspace + (size_t)tiles * a.parts * kRows * 64 * 4);
   const float c = sm_scale * 1.4426950408889634f;
