@@ -19,6 +19,9 @@ constexpr int kWaves = 4;
 constexpr int kBlock = LITEVAR_KV8_BLOCK;      // keys per turn
 constexpr int kPitch = 68;                     // floats per row of the joining buffer
 
+// An exponent that is added to a reference beyond this loses bits that show (codes: the V scales; see k_cross_tiles).
+constexpr float kFarCodes = 0x1p12f;
+
 enum Kind { kBf16 = 0, kF32 = 1, kCodes = 2 };
 
 struct CrossArgs {
@@ -44,6 +47,9 @@ __device__ inline Row row_at(const CrossArgs& a, int j, int r) {
 }
 
 __device__ inline int keys_of(const CrossArgs& a, int b) { return a.len ? min(max(a.len[b], 0), a.kv_len) : a.kv_len; }
+
+// a value that is the same in all lanes, in a scalar register
+__device__ inline float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
 
 // eight codes (a word pair) as bf16, exactly
 __device__ inline bf16x8 codes_to_bf16(unsigned lo, unsigned hi) {
@@ -288,25 +294,73 @@ __global__ __launch_bounds__(kWaves * 64) void k_cross_rows(CrossArgs a, float c
   store_row<KIND>(a, b, j, row0 + row, dims, x);
 }
 
+// One row, by all 64 lanes of a wave and behind its store: a score per lane, 64 keys at a time, then lane d dimension d.
+// The largest score is subtracted before the scale is applied.
+template <int KIND>
+__device__ inline void row_again(const CrossArgs& a, float c, int b, int j, int bj, int n_keys, int row) {
+  wait_vmcnt<0>();
+  const int lane = lane_of_wave();
+  const Row qr = row_at(a, j, row);
+  const __bf16* q = (const __bf16*)a.q + b * a.qs[0] + qr.h * a.qs[1] + qr.i * a.qs[2];
+  const int64_t kv_at = b * a.ks[0] + j * a.ks[1];
+  float m = -INFINITY, l = 0.f, o = 0.f;
+  for (int key0 = 0; key0 < n_keys; key0 += 64) {
+    const int64_t at = kv_at + min(key0 + lane, n_keys - 1) * a.ks[2];
+    const int64_t scale_at = KIND == kCodes ? (int64_t)bj * a.scale_blocks + key0 / kBlock : 0;
+    float s = 0.f;
+#pragma unroll 1
+    for (int d = 0; d < 64; d += 8) {
+      bf16x8 x;
+      if constexpr (KIND == kCodes) {
+        const uint2 w = *(const uint2*)((const int8_t*)a.k + at + d);
+        x = codes_to_bf16(w.x, w.y);
+      } else {
+        x = as_bf16x8(*(const uint4*)((const __bf16*)a.k + at + d));
+      }
+      const bf16x8 y = as_bf16x8(*(const uint4*)(q + d));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = fmaf((float)x[e], (float)y[e], s);
+    }
+    float vs = 1.f;
+    if constexpr (KIND == kCodes) { s *= a.k_scale[scale_at]; vs = a.v_scale[scale_at]; }
+    s = key0 + lane < n_keys ? s : -INFINITY;
+    float mx = s;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
+    const float to = fmaxf(m, mx);
+    const float alpha = m > -INFINITY ? __builtin_amdgcn_exp2f((m - to) * c) : 0.f;
+    const float p = __builtin_amdgcn_exp2f((s - to) * c);
+    float sum = p;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    l = fmaf(l, alpha, sum); o *= alpha; m = to;
+    for (int i = 0; i < min(64, n_keys - key0); ++i) {
+      const int64_t v_at = kv_at + (int64_t)(key0 + i) * a.ks[2] + lane;
+      const float v = KIND == kCodes ? (float)((const int8_t*)a.v)[v_at] * vs : (float)((const __bf16*)a.v)[v_at];
+      o = fmaf(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(p), i)), v, o);
+    }
+  }
+  ((__bf16*)a.o + b * a.os[0] + qr.h * a.os[1] + qr.i * a.os[2])[lane] = (__bf16)(o * (1.f / l));
+}
+
 // Many rows: NWV waves of one (batch, kv head), each with 32 rows, share the K and V rows, which pass through LDS in chunks
 // of 64 keys, three buffers: one read, one landing, one whose last readers may be behind, so that one barrier per chunk
 // is enough.  bf16 rows come by LDS-DMA; codes through registers, converted (exactly) on their way, one chunk ahead.  The
 // score products of a block of 32 keys are issued ahead of the exponentials of the block before it.
 //
-// Softmax in base 2: the reference is the largest score of the first block and moves when a sum passes 2^10, so that no
-// maximum is formed in the other blocks.  p = exp2(s c - m c) in one instruction where |m c| < 2^13 (beyond it the rounding
-// of m c would show; there the reference is subtracted before the scale is applied).
+// Softmax in base 2: the reference is the largest score of the first block and moves (by whole powers of two) when a sum
+// passes 2^40, so that no maximum is formed in the other blocks.  Rows whose reference went beyond kFarReference, where its
+// rounding would show, and rows that overflowed are formed again behind the store.
 //
 // Codes: a chunk is a block, its K scale joins the softmax scale.  Its V scale, relative to the largest of the
 // keys that count, is added to the exponent, which costs nothing per score; the chunk's part of the row sum is divided by it
 // again.  (Relative V scales are taken as at least 2^-96, so that no probability that counts is flushed to zero.)
-template <int NWV, int KIND>
-__global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(NWV == 4 ? 3 : 4, NWV == 4 ? 3 : 4)))
+template <int NWV, int BUFS, int KIND>
+__global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(NWV == 4 && BUFS == 3 ? 3 : 4, NWV == 4 && BUFS == 3 ? 3 : 4)))
 void k_cross_tiles(CrossArgs a, float c) {
   constexpr bool CODES = KIND == kCodes;
   constexpr int kRowsPerWave = kBlock / NWV, kTransfers = kRowsPerWave / 8, kBuf = 2 * kBlock * kRow;
-  constexpr float kMost = 0x1p10f, kFar = 0x1p13f;
-  __shared__ __align__(1024) unsigned char smem[3 * kBuf];
+  __shared__ __align__(1024) unsigned char smem[BUFS * kBuf];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int n = lane & 31, hh = lane >> 5;
   // all (batch, kv head) pairs of one tile next to each other: workgroup i runs on XCD i % 8, so the tiles of a pair share
@@ -317,9 +371,9 @@ void k_cross_tiles(CrossArgs a, float c) {
   const int n_keys = keys_of(a, b);
   const int row0 = (tile * NWV + wave) * kRows;
   const bool working = row0 < a.rows;          // (uniform)
-  const Row qr = row_at(a, j, min(row0 + n, a.rows - 1));    // (a column without a row holds the last one; it is not stored)
   bf16x8 qf[4];
   {
+    const Row qr = row_at(a, j, min(row0 + n, a.rows - 1));    // (a column without a row holds the last one; it is not stored)
     const __bf16* qp = (const __bf16*)a.q + b * a.qs[0] + qr.h * a.qs[1] + qr.i * a.qs[2] + 8 * hh;
 #pragma unroll
     for (int t = 0; t < 4; ++t) qf[t] = as_bf16x8(*(const uint4*)(qp + 16 * t));
@@ -331,14 +385,17 @@ void k_cross_tiles(CrossArgs a, float c) {
   const int64_t kv_at = b * a.ks[0] + j * a.ks[1];
   const int lrow = lane >> 3;
   const unsigned piece_off = (((unsigned)lane & 7u) ^ dense_swizzle((unsigned)lrow)) << 4;
+  [[maybe_unused]] const unsigned row_bytes = (unsigned)a.ks[2] * 2u;
   [[maybe_unused]] auto issue_chunk = [&](int chunk, int buf) {
 #pragma unroll
     for (int i = 0; i < kTransfers; ++i) {
-      const int r0 = kRowsPerWave * wave + 8 * i, key = min(kBlock * chunk + r0 + lrow, n_keys - 1);
-      const int64_t src = (kv_at + key * a.ks[2]) * 2 + piece_off;
+      // (a scalar base per chunk and 32-bit offsets inside it: 64 rows span less than 4 GiB, checked by the launch)
+      const int r0 = kRowsPerWave * wave + 8 * i, key = min(r0 + lrow, n_keys - 1 - kBlock * chunk);
+      const int64_t base = (kv_at + (int64_t)chunk * kBlock * a.ks[2]) * 2;
+      const unsigned src = (unsigned)key * row_bytes + piece_off;
       unsigned char* dst = smem + buf * kBuf + r0 * kRow;
-      __builtin_amdgcn_global_load_lds((global_void*)((const unsigned char*)a.k + src), (lds_void*)dst, 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((global_void*)((const unsigned char*)a.v + src), (lds_void*)(dst + kBlock * kRow), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((global_void*)((const unsigned char*)a.k + base + src), (lds_void*)dst, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((global_void*)((const unsigned char*)a.v + base + src), (lds_void*)(dst + kBlock * kRow), 16, 0, 0);
     }
   };
   // codes: 16 of a K or V row per thread and piece, 512 pieces to a chunk
@@ -347,8 +404,9 @@ void k_cross_tiles(CrossArgs a, float c) {
   [[maybe_unused]] auto load_chunk = [&](int chunk) {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int at = tid + NWV * 64 * i, key = min(kBlock * chunk + ((at & 255) >> 2), n_keys - 1);
-      codes[i] = *(const u32x4*)((const int8_t*)(at < 256 ? a.k : a.v) + kv_at + (int64_t)key * 64 + 16 * (at & 3));
+      const int at = tid + NWV * 64 * i, key = min((at & 255) >> 2, n_keys - 1 - kBlock * chunk);
+      const int8_t* base = (const int8_t*)(wave + NWV * i < 4 ? a.k : a.v) + kv_at + (int64_t)chunk * (kBlock * 64);
+      codes[i] = *(const u32x4*)(base + (unsigned)(key * 64 + 16 * (at & 3)));
     }
   };
   [[maybe_unused]] auto commit_chunk = [&](int buf) {
@@ -361,13 +419,12 @@ void k_cross_tiles(CrossArgs a, float c) {
       *(bf16x8*)(dst + (((p + 1u) ^ sw) << 4)) = codes_to_bf16(codes[i][2], codes[i][3]);
     }
   };
-  // scales of 64 chunks at a time, lane i chunk i's: K's, log2 of V's over the largest, and its inverse
-  [[maybe_unused]] float vmax = 0.f, my_ks = 1.f, my_lv = 0.f, my_iv = 1.f;
+  // a chunk's scales, as scalar loads (requested half a chunk ahead), and log2 of the largest V scale
+  [[maybe_unused]] float vmax = 0.f, log_vmax = 0.f;
+  [[maybe_unused]] int ks_bits = 0, vs_bits = 0;
   [[maybe_unused]] auto load_scales = [&](int chunk) {
-    const int64_t at = (int64_t)bj * a.scale_blocks + min(chunk + lane, n_chunks - 1);
-    my_ks = a.k_scale[at];
-    const float vs = a.v_scale[at], rel = vs > 0.f && vmax > 0.f ? fmaxf(vs / vmax, 0x1p-96f) : 1.f;
-    my_lv = __builtin_amdgcn_logf(rel); my_iv = 1.f / rel;         // (base 2)
+    const int64_t at = (int64_t)bj * a.scale_blocks + chunk;
+    ks_bits = ((const_i32_ptr)a.k_scale)[at]; vs_bits = ((const_i32_ptr)a.v_scale)[at];
   };
 
   // LDS read offsets: K piece 2 t + hh of row n; V: 4 keys x 16 dims per 16 lanes
@@ -383,10 +440,11 @@ void k_cross_tiles(CrossArgs a, float c) {
   }
 
   f32x16 O[2] = {f32x16{}, f32x16{}};
-  float L[2] = {0.f, 0.f}, m = 0.f, negm = 0.f;          // this lane's part of the row sum; the reference, and minus it in base 2
+  float L[2] = {0.f, 0.f}, negm = 0.f;         // this lane's part of the row sum, one chain per slice; minus the reference (base 2)
   bool unset = true;
-  uint64_t far = 0;
+  uint64_t far = 0;                            // lanes whose reference has been beyond kFar
 
+  auto is_beyond = [](float x) { return __builtin_amdgcn_ballot_w64(!(fabsf(x) < (CODES ? kFarCodes : kFarReference))); };
   auto scores = [&](u32x4 (&kr)[4]) -> f32x16 {
     lds_wait_k(kr[0], kr[1], kr[2], kr[3]);
     f32x16 S = f32x16{};
@@ -402,39 +460,31 @@ void k_cross_tiles(CrossArgs a, float c) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) S[e] = 8 * (e >> 2) + (e & 3) < left ? S[e] : -INFINITY;
     }
-    auto largest = [&]() {                     // score of the row, over both of its lanes
-      float mx = S[0];
-#pragma unroll
-      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, S[e]);
-      return fmaxf(mx, other_half(mx)) * ks;
-    };
-    auto set_reference = [&](float to) {
-      m = to; negm = -m * c;
-      far |= __builtin_amdgcn_ballot_w64(!(fabsf(negm) < kFar));
-    };
     if (CODES && ks < 0x1p-100f) {             // (a block of zeros or nearly so: scaled here, c ks would lose its bits)
 #pragma unroll
       for (int e = 0; e < 16; ++e) S[e] = S[e] > -INFINITY ? S[e] * ks : S[e];
       ks = 1.f;
     }
-    if (unset) { set_reference(largest()); unset = false; }
+    auto largest = [&]() {                     // of the row, over both of its lanes
+      float mx = S[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, S[e]);
+      return fmaxf(mx, other_half(mx));
+    };
+    const float cb = CODES ? c * ks : c;
+    if (unset) {
+      negm = -largest() * cb; unset = false;
+      far = is_beyond(negm);
+    }
     bf16x8 pb[2];
     float sum[2];
     auto exponentials = [&]() {
-      const float cb = CODES ? c * ks : c, at = CODES ? negm + lv : negm;
+      const float at = CODES ? negm + lv : negm;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         sum[t] = CODES ? 0.f : L[t];
-        if (__builtin_expect(far != 0, 0)) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float d = CODES ? __builtin_fmaf(S[8 * t + e], ks, -m) : S[8 * t + e] - m;
-            pb[t][e] = (__bf16)__builtin_amdgcn_exp2f(CODES ? __builtin_fmaf(d, c, lv) : d * c);
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) pb[t][e] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(S[8 * t + e], cb, at));
-        }
+        for (int e = 0; e < 8; ++e) pb[t][e] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(S[8 * t + e], cb, at));
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
           const bf16x2 two = {pb[t][e], pb[t][e + 1]};
@@ -444,15 +494,14 @@ void k_cross_tiles(CrossArgs a, float c) {
       }
     };
     exponentials();
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(fmaxf(sum[0], sum[1]) > kMost) != 0, 0)) {
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(fmaxf(sum[0], sum[1]) > kMostSum) != 0, 0)) {
       auto both = [&](const float (&x)[2]) { const float y = x[0] + x[1]; return y + other_half(y); };   // slices, lanes
       const float now = both(sum), before = both(L);
-      float to = fmaxf(m, largest());
-      if (before > 1.f) to = fmaxf(to, m + __builtin_amdgcn_logf(before) / c);
-      to = now > kMost ? to : m;
-      const float alpha = __builtin_amdgcn_exp2f((m - to) * c);
-      set_reference(to);
-      L[0] *= alpha; L[1] *= alpha;
+      float to = __builtin_fmaf(largest(), cb, negm);
+      if (before > 0.f) to = fmaxf(to, __builtin_amdgcn_logf(before));         // (base 2)
+      const float shift = now > kMostSum ? rintf(to) : 0.f, alpha = __builtin_amdgcn_exp2f(-shift);
+      negm -= shift; L[0] *= alpha; L[1] *= alpha;
+      far |= is_beyond(negm);
 #pragma unroll
       for (int e = 0; e < 16; ++e) { O[0][e] *= alpha; O[1][e] *= alpha; }
       exponentials();
@@ -474,6 +523,9 @@ void k_cross_tiles(CrossArgs a, float c) {
       for (int at = 0; at < n_chunks; at += 64) vmax = fmaxf(vmax, a.v_scale[(int64_t)bj * a.scale_blocks + min(at + lane, n_chunks - 1)]);
 #pragma unroll
       for (int d = 32; d > 0; d >>= 1) vmax = fmaxf(vmax, __shfl_xor(vmax, d));
+      vmax = uniform(vmax);
+      log_vmax = uniform(__builtin_amdgcn_logf(vmax));
+      load_scales(0);
       commit_chunk(0);
       if (n_chunks > 1) load_chunk(1);
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -493,15 +545,15 @@ void k_cross_tiles(CrossArgs a, float c) {
     // blocks the next chunk is made sure of and the one after it requested, for the buffer that every wave has read to
     // its end by then.
     auto one = [&](int chunk, auto which) -> bool {
-      constexpr int p = decltype(which)::value, AT = p * kBuf, NEXT = (p + 1) % 3 * kBuf;
+      constexpr int p = decltype(which)::value, AT = p * kBuf, NEXT = (p + 1) % BUFS * kBuf;
       const int key0 = chunk * kBlock;
       const bool more = chunk + 1 < n_chunks, second = key0 + 32 < n_keys;
       float ks = 1.f, lv = 0.f, iv = 1.f;
       if constexpr (CODES) {
-        if ((chunk & 63) == 0) load_scales(chunk);
-        ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_ks), chunk & 63));
-        lv = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_lv), chunk & 63));
-        iv = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_iv), chunk & 63));
+        // (a scale of zero belongs to a block of zeros: any will do)
+        ks = __int_as_float(ks_bits);
+        lv = uniform(__int_as_float(vs_bits) > 0.f ? fmaxf(__builtin_amdgcn_logf(__int_as_float(vs_bits)) - log_vmax, -96.f) : 0.f);
+        iv = uniform(__builtin_amdgcn_exp2f(-lv));
       }
       f32x16 S1;
       asm volatile("" : "=v"(S1));             // (not set where there is no second block, and not used then)
@@ -518,13 +570,14 @@ void k_cross_tiles(CrossArgs a, float c) {
       }
       if (more) {
         if constexpr (CODES) {
-          commit_chunk((p + 1) % 3);
+          commit_chunk((p + 1) % BUFS);
           if (chunk + 2 < n_chunks) load_chunk(chunk + 2);
+          load_scales(chunk + 1);
           asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         } else {
           wait_vmcnt<0>();
           asm volatile("s_barrier" ::: "memory");
-          if (chunk + 2 < n_chunks) issue_chunk(chunk + 2, (p + 2) % 3);
+          if (BUFS == 3 && chunk + 2 < n_chunks) issue_chunk(chunk + 2, (p + 2) % BUFS);
         }
       }
       if (working && second) {
@@ -538,12 +591,18 @@ void k_cross_tiles(CrossArgs a, float c) {
         __builtin_amdgcn_sched_barrier(0);
         absorb(S1, va, key0 + 32, ks, lv, iv);
       }
+      if (BUFS == 2 && chunk + 2 < n_chunks) {
+        asm volatile("s_barrier" ::: "memory");
+        issue_chunk(chunk + 2, p);
+      }
       return more;
     };
-    for (int chunk = 0;; chunk += 3) {
+    for (int chunk = 0;; chunk += BUFS) {
       if (!one(chunk, std::integral_constant<int, 0>{})) break;
       if (!one(chunk + 1, std::integral_constant<int, 1>{})) break;
-      if (!one(chunk + 2, std::integral_constant<int, 2>{})) break;
+      if constexpr (BUFS == 3) {
+        if (!one(chunk + 2, std::integral_constant<int, 2>{})) break;
+      }
     }
   }
 
@@ -558,8 +617,13 @@ void k_cross_tiles(CrossArgs a, float c) {
       if constexpr (CODES) { x *= unit; y *= unit; }
       r[dt][e / 2] = __builtin_bit_cast(unsigned, bf16x2{(__bf16)x, (__bf16)y});
     }
-  if (row0 + n < a.rows) {
-    __bf16* op = (__bf16*)a.o + b * a.os[0] + qr.h * a.os[1] + qr.i * a.os[2] + 8 * hh;
+  float any = 0.f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) any = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, r[e >> 3][e & 7]), kOnes, any, false);
+  int row = row0 + (lane_of_wave() & 31);      // (formed anew: not worth registers through the loop)
+  if (row < a.rows) {
+    const Row qr = row_at(a, j, row);
+    __bf16* op = (__bf16*)a.o + b * a.os[0] + qr.h * a.os[1] + qr.i * a.os[2] + 8 * (lane_of_wave() >> 5);
 #pragma unroll
     for (int dt = 0; dt < 2; ++dt)
 #pragma unroll
@@ -571,6 +635,10 @@ void k_cross_tiles(CrossArgs a, float c) {
         *(u32x4*)(op + 32 * dt + 16 * jj) = piece;
       }
   }
+  // Rows whose reference went too far, and rows whose products with V overflowed under a sum that had been let grow.
+  uint64_t bad = (far | __builtin_amdgcn_ballot_w64(not_finite(any))) & __builtin_amdgcn_ballot_w64(row < a.rows);
+  bad = (bad | (bad >> 32)) & 0xffffffffull;
+  for (; __builtin_expect(bad != 0, 0); bad &= bad - 1) row_again<KIND>(a, c, b, j, bj, n_keys, row0 + __builtin_ctzll(bad));
 }
 
 // Joins the parts of one tile of rows: a workgroup per (batch, kv head, tile).
@@ -632,12 +700,13 @@ litevar_status strides_of(const int64_t* s, int B, int heads, int64_t n, int D, 
 template <int KIND> litevar_status launch(CrossArgs& a, float c, hipStream_t st) {
   const int64_t tiles = (int64_t)a.B * a.Hkv * a.tiles;
   if constexpr (KIND != kF32) {
-    if (a.parts == 1 && a.tiles > 1) {
-      const int nwv = a.tiles > 4 ? 8 : 4;
+    // (64 rows of K or V span less than 4 GiB, see issue_chunk)
+    if (a.parts == 1 && a.tiles > 1 && a.ks[2] < (1 << 24)) {
+      const int nwv = KIND != kCodes && a.tiles > 4 ? 8 : 4;
       return launch_in_parts((int64_t)a.B * a.Hkv * ((a.tiles + nwv - 1) / nwv), nwv * 64, "cross attention launch", [&](int64_t first, unsigned n) {
         a.first_block = (uint32_t)first;
-        if (nwv == 8) hipLaunchKernelGGL((k_cross_tiles<8, KIND>), dim3(n), dim3(512), 0, st, a, c);
-        else hipLaunchKernelGGL((k_cross_tiles<4, KIND>), dim3(n), dim3(256), 0, st, a, c);
+        if (nwv == 8) hipLaunchKernelGGL((k_cross_tiles<8, 3, kBf16>), dim3(n), dim3(512), 0, st, a, c);
+        else hipLaunchKernelGGL((k_cross_tiles<4, 3, KIND>), dim3(n), dim3(256), 0, st, a, c);
       });
     }
   }
