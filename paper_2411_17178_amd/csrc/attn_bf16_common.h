@@ -2,10 +2,14 @@
 // transposing LDS read, lane-mask select, the cross-row maximum and the LDS / vmcnt
 // primitives that must not wait for outstanding LDS-DMA loads.
 #pragma once
+#include <type_traits>
+
 #include "internal.h"
 
 namespace lv {
 
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
@@ -135,33 +139,44 @@ __device__ inline int lane_of_wave() { return (int)__builtin_amdgcn_mbcnt_hi(~0u
 // Bound: about 400 instructions and two trips to memory for 32 keys.  2240 tokens, 288 pairs, a bad V element in a token
 // that all queries keep, K all NaN, a bad V element in a late token: 1.3 / 0.9 / 3.2 ms a call (with a row per lane, key
 // by key and to the end: 10.8 / 12.9 / 2.9).
-template <bool Q8, class Keys>
+// KV: bf16 queries on an 8-bit cache with block scales; values as they are, in fp32.
+template <bool Q8, bool KV, class Keys, class Scales>
 __device__ inline void attend_row(const AttnArgs& a, float c, int b, int h, int qrow, bool shared, bool mine,
-                                  const Keys keys) {
+                                  const Keys keys, [[maybe_unused]] const Scales& scales) {
   constexpr int kElem = Q8 ? 1 : 2;
   const int lane = lane_of_wave(), i = lane & 31, first_dim = lane & 32;
   const int64_t kv_at = (b * a.ks[0] + h * a.ks[1]) * kElem, pair = (int64_t)b * a.H + h;
   const unsigned char *K = (const unsigned char*)a.k + kv_at, *V = (const unsigned char*)a.v + kv_at;
-  const unsigned row_bytes = (unsigned)a.ks[2] * kElem;    // (a (batch, head) slab spans < 2 GiB)
+  unsigned row_bytes = (unsigned)a.ks[2] * kElem;          // (a (batch, head) slab spans < 2 GiB)
   [[maybe_unused]] const int64_t first_row = Q8 ? pair * (a.ks[1] / a.ks[2]) : 0;
+  if constexpr (KV) {
+    K = (const unsigned char*)scales.k8 + pair * a.kv_len * 64; V = (const unsigned char*)scales.v8 + pair * a.kv_len * 64;
+    row_bytes = 64;
+  }
   qrow = checked_index(a.hdr, qrow, a.q_len);
-  // 32 dimensions of a row: bf16, or 8-bit codes with the row's (scale, zero point) as the kernels convert them
-  auto load_half = [&](const unsigned char* row, [[maybe_unused]] const float2* sz, float (&x)[32]) {
-    const u32x4* p = (const u32x4*)(row + first_dim * kElem);
-    u32x4 raw[2 * kElem];
+  // 32 dimensions of a row: bf16, or 8-bit codes with the row's (scale, zero point) as the kernels convert them, or with
+  // a block's scale
+  auto load_half = [&](const unsigned char* row, [[maybe_unused]] const float2* sz, float (&x)[32], auto is_code,
+                       [[maybe_unused]] float scale) {
+    constexpr bool CODE = decltype(is_code)::value;
+    constexpr int kBytes = CODE ? 1 : 2;
+    const u32x4* p = (const u32x4*)(row + first_dim * kBytes);
+    u32x4 raw[2 * kBytes];
 #pragma unroll
-    for (int t = 0; t < 2 * kElem; ++t) raw[t] = p[t];
+    for (int t = 0; t < 2 * kBytes; ++t) raw[t] = p[t];
     float2 f = make_float2(0.f, 0.f);
     if constexpr (Q8) f = *sz;
 #pragma unroll
     for (int e = 0; e < 32; ++e) {
-      if constexpr (Q8) x[e] = (float)(__bf16)fmaf(f.x, (float)(int8_t)((raw[e >> 4][(e >> 2) & 3] >> (8 * (e & 3))) & 0xffu), f.y);
+      [[maybe_unused]] const float code = (float)(int8_t)((raw[e >> (CODE ? 4 : 3)][(e >> 2) & 3] >> (8 * (e & 3))) & 0xffu);
+      if constexpr (Q8) x[e] = (float)(__bf16)fmaf(f.x, code, f.y);
+      else if constexpr (CODE) x[e] = scale * code;
       else x[e] = __uint_as_float(e & 1 ? raw[e >> 3][(e >> 1) & 3] & 0xffff0000u : raw[e >> 3][(e >> 1) & 3] << 16);
     }
   };
   float q[32];
   load_half((const unsigned char*)a.q + (b * a.qs[0] + h * a.qs[1] + qrow * a.qs[2]) * kElem,
-            Q8 ? a.q_sz + pair * a.q_len + qrow : nullptr, q);
+            Q8 ? a.q_sz + pair * a.q_len + qrow : nullptr, q, std::integral_constant<bool, Q8>{}, 1.f);
   float m = -INFINITY, l = 0.f, o = 0.f;
   bool nan = false;                            // a kept key's score is
   for (int block = 0; block < keys.n_blocks; ++block) {
@@ -171,7 +186,13 @@ __device__ inline void attend_row(const AttnArgs& a, float c, int b, int h, int 
     if (kept == 0) continue;
     tok = checked_index(a.hdr, keep ? tok : __builtin_amdgcn_readlane(tok, __builtin_ctz(kept)), a.kv_len);
     float dot = 0.f, x[32];
-    load_half(K + (unsigned)tok * row_bytes, Q8 ? a.k_sz + first_row + tok : nullptr, x);
+    float k_scale = 1.f;
+    [[maybe_unused]] float v_scale = 1.f;
+    if constexpr (KV) {
+      const int64_t at = pair * scales.n_blocks + scales.block_of(tok, a.n_scales);
+      k_scale = scales.k[at]; v_scale = scales.v[at];
+    }
+    load_half(K + (unsigned)tok * row_bytes, Q8 ? a.k_sz + first_row + tok : nullptr, x, std::integral_constant<bool, Q8 || KV>{}, k_scale);
 #pragma unroll
     for (int e = 0; e < 32; ++e) dot = fmaf(q[e], x[e], dot);
     dot += __shfl_xor(dot, 32);
@@ -199,6 +220,8 @@ __device__ inline void attend_row(const AttnArgs& a, float c, int b, int h, int 
         if constexpr (Q8) {
           const float2 f = a.v_sz[first_row + t];
           v[j] = (float)(__bf16)fmaf(f.x, (float)((const int8_t*)row)[lane], f.y);
+        } else if constexpr (KV) {
+          v[j] = (float)((const int8_t*)row)[lane] * __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale), j0 + j));
         } else {
           v[j] = (float)((const __bf16*)row)[lane];
         }
@@ -230,15 +253,17 @@ __device__ inline unsigned not_finite_dims(const unsigned (&r)[2][8]) {
 
 // attend_row for the rows of the lanes in `rows` (their row: `row`), behind the store of the wave's results: the
 // dimensions dims of a lane and of the one 32 above it are stored again.
-template <bool Q8, class KeysOf>
-__device__ inline void attend_rows(const AttnArgs& a, float c, int b, int h, bool shared, unsigned rows, int row, unsigned dims, KeysOf keys_of) {
+struct NoScales {};
+template <bool Q8, bool KV = false, class KeysOf, class Scales = NoScales>
+__device__ inline void attend_rows(const AttnArgs& a, float c, int b, int h, bool shared, unsigned rows, int row, unsigned dims, KeysOf keys_of,
+                                   const Scales& scales = {}) {
   for (; __builtin_expect(rows != 0, 0); rows &= rows - 1) {
     wait_vmcnt<0>();                           // (what is stored next goes to places that were just stored to)
     const int at = __builtin_ctz(rows), r = __builtin_amdgcn_readlane(row, at), l = lane_of_wave();
     // lane d for dimension d: value 16 (d / 32) + 4 (d / 8 % 4) + d % 4 of the query's lane half d / 4 % 2
     const unsigned lo = __builtin_amdgcn_readlane(dims, at), up = __builtin_amdgcn_readlane(dims, at + 32);
     const bool mine = ((l & 4 ? up : lo) >> (16 * (l >> 5) + 4 * ((l >> 3) & 3) + (l & 3))) & 1u;
-    attend_row<Q8>(a, c, b, h, r, shared, mine, keys_of(r));
+    attend_row<Q8, KV>(a, c, b, h, r, shared, mine, keys_of(r), scales);
   }
 }
 
@@ -343,5 +368,35 @@ __device__ inline void read_v(const unsigned (&v)[2], u32x2 (&va)[8]) {
                  "=&v"(va[4]), "=&v"(va[5]), "=&v"(va[6]), "=&v"(va[7])
                : "v"(v[0]), "v"(v[1]), "i"(AT), "i"(AT + 8 * kRow), "i"(AT + 16 * kRow), "i"(AT + 24 * kRow) : "memory");
 }
+
+// ---- 8-bit cache in f16 ----
+// The power of two that brings x to [2^13, 2^14).
+__device__ inline int power_to_14(float x) { return x > 0.f ? 14 - __builtin_amdgcn_frexp_expf(x) : 0; }
+
+template <int kCtrl> __device__ inline float dpp_row(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), kCtrl, 0xf, 0xf, true));
+}
+// the largest value of the wave, in a scalar register
+__device__ inline float wave_max(float x) {
+  x = fmaxf(x, dpp_row<0xb1>(x));              // lane ^ 1
+  x = fmaxf(x, dpp_row<0x4e>(x));              // lane ^ 2
+  x = fmaxf(x, dpp_row<0x141>(x));             // lane i <- 7 - i of its eight
+  x = fmaxf(x, dpp_row<0x140>(x));             // lane i <- 15 - i of its sixteen
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(max_across_rows(x))));
+}
+
+// The block scales of a (batch, head), dealt to the lanes of a wave: power() brings 127 times the largest finite one
+// below 2^14; wide(): one that is not zero lies more than 2^20 below it.
+struct HeadScales {
+  float largest = 0.f, least = INFINITY;       // of this lane's, and of the whole head behind join()
+  __device__ void add(float x) {
+    const bool counts = !not_finite(x);
+    largest = counts ? fmaxf(largest, x) : largest;
+    least = counts && x > 0.f ? fminf(least, x) : least;
+  }
+  __device__ void join() { largest = wave_max(largest); least = -wave_max(-least); }
+  __device__ int power() const { return largest > 0x1p120f ? power_to_14(largest) - 7 : power_to_14(127.f * largest); }
+  __device__ bool wide() const { return least < largest * 0x1p-20f; }
+};
 
 }  // namespace lv

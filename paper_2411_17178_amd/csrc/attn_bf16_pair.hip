@@ -128,13 +128,30 @@ __device__ inline void lds_read_v_wide(const unsigned (&v)[4], const unsigned (&
                : "v"(v[0]), "v"(x[0]), "v"(v[1]), "v"(x[1]), "v"(v[2]), "v"(x[2]), "v"(v[3]), "v"(x[3]),
                  "i"(VOFF) : "memory");
 }
+constexpr f16x2 kHalfOnes = {(_Float16)1.0f, (_Float16)1.0f};
+
+__device__ inline f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ inline f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+// Eight codes times s, rounded to f16 once.  (The scale itself rounded to f16 would move all scores of a block alike: with
+// scores of +-100 a weight was off by 3 % that way.)
+__device__ inline f16x8 codes_to_f16(unsigned lo, unsigned hi, float s) {
+  f16x8 r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = (_Float16)(s * (float)(int8_t)(((e < 4 ? lo : hi) >> (8 * (e & 3))) & 0xffu));
+  return r;
+}
+
+__device__ inline int64_t scales_blocks(const KV8Scales& s) { return s.n_blocks; }
+__device__ inline int64_t scales_blocks(const NoScales&) { return 0; }
+
 struct WideArgs {
   const WaveDesc* waves;  // the wide patches
   int boost;              // all workgroups of the launch are resident at once
 };
 
-struct WidePatchState {   // a wave's 32 queries
-  bf16x8 q[4];            // Q^T as the B operand: lane (n, h) holds Q[query n][16 t + 8 h .. + 7]
+template <class E8> struct WidePatchState {   // a wave's 32 queries
+  E8 q[4];                // Q^T as the B operand: lane (n, h) holds Q[query n][16 t + 8 h .. + 7]
   f32x16 O[2];            // O^T accumulators: dims 32 dt + 8 (e / 4) + 4 h + e % 4 of query n
   float L, negm;          // this lane's part of the row sum, minus the softmax reference m (base 2, whole numbers)
   uint64_t unset;         // lanes whose query's sum is still below kLeastSum
@@ -188,9 +205,23 @@ struct StepKeys {
 // slots, same swizzle -- at the end of the phase, before the barrier.  Steps, masks and
 // epilogue are the same code; the ring holds exactly what a dequantised bf16 copy would put
 // there, so the results equal those of the bf16 kernel on such a copy bit for bit.
-template <int PW, bool Q8>
+//
+// KV (an 8-bit cache with block scales, bf16 queries): the products run on f16.  A head's K values are multiplied by the
+// power of two that puts its largest block scale near 2^7 (values below 2^14), V's likewise, every query by its own; the
+// powers leave through the softmax scale of the lane and the stored result.  f16 holds three bits more than bf16: a code
+// times its scale is off by 2^-12 at most, a probability by 2^-11 (towards zero, in the sum and the products alike; weights
+// below 2^-11 of the row's sum by up to 2^-21 of it, where f16 is subnormal).  With bf16 in their place the result was off by 0.0033
+// relative to its norm, by 0.0018 so; the store's own rounding is 0.0017.  Heads whose block scales differ by more than 2^20
+// would lose bits of the smaller blocks: all their rows are formed again from the codes.
+//   KV = 1: K and V are copies in f16 (k_kv8_copy), which come by LDS-DMA.
+//   KV = 2: the codes are converted on their way into LDS, as with Q8.
+template <int PW, bool Q8, int KV = 0>
 __global__ __launch_bounds__((kGroupPatches / PW) * 64) __attribute__((amdgpu_waves_per_eu(4, 4)))
-void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c) {
+void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV != 0, KV8Scales, NoScales> scales) {
+  static_assert(KV == 0 || (PW == 2 && !Q8), "the cache's forms have wide patches");
+  constexpr bool CODES = Q8 || KV == 2;            // K and V come through registers
+  using E8 = std::conditional_t<KV != 0, f16x8, bf16x8>;
+  [[maybe_unused]] constexpr float kMost = KV ? 0x1p15f : kMostSum, kLeast = KV ? 0x1p-3f : kLeastSum;
   constexpr bool WIDE = PW == 2;                   // the group's wide patches (32 queries), else its patches (16)
   constexpr int C = kDmaKeys;
   constexpr int R = kRingChunks * C;               // ring slots
@@ -237,13 +268,13 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c) {
 
   // ---- loading duty: rows [8 w, 8 w + 8) of every chunk, w = wave mod 8: K and V rows with
   // eight waves, K rows (waves 0-7) or V rows (waves 8-15) with sixteen ----
-  constexpr int kElem = Q8 ? 1 : 2;                    // bytes per operand element
-  const unsigned char* Kp = (const unsigned char*)a.k + (b * a.ks[0] + h * a.ks[1]) * kElem;
-  const unsigned char* Vp = (const unsigned char*)a.v + (b * a.ks[0] + h * a.ks[1]) * kElem;
-  const unsigned row_bytes = (unsigned)a.ks[2] * kElem;   // a (batch, head) slab spans < 2 GiB (checked by the API)
+  constexpr int kElem = Q8 ? 1 : 2, kKvElem = CODES ? 1 : 2;      // bytes per element of Q, of K and V
+  const unsigned char* Kp = (const unsigned char*)a.k + (b * a.ks[0] + h * a.ks[1]) * kKvElem;
+  const unsigned char* Vp = (const unsigned char*)a.v + (b * a.ks[0] + h * a.ks[1]) * kKvElem;
+  const unsigned row_bytes = (unsigned)a.ks[2] * kKvElem; // a (batch, head) slab spans < 2 GiB (checked by the API)
   const int32_t* utok = a.union_tok + gd.union_base;
-  // bf16: eight lanes per 128-byte row; Q8: four lanes per 64-byte row of codes
-  const int row = Q8 ? 8 * (wave & 7) + ((lane >> 2) & 7) : 8 * (wave & 7) + (lane >> 3);
+  // bf16: eight lanes per 128-byte row; codes: four lanes per 64-byte row
+  const int row = CODES ? 8 * (wave & 7) + ((lane >> 2) & 7) : 8 * (wave & 7) + (lane >> 3);
   // A lane's row of chunk t goes to slot (t % 5) * 64 + row.  Chunks start at multiples of 64
   // slots, so the slot's swizzle -- and with it the 16-byte piece of the source row that
   // this lane fetches -- does not depend on t.
@@ -260,7 +291,36 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c) {
       __builtin_amdgcn_global_load_lds((global_void*)(Vp + src), (lds_void*)(Vring + slot0 * kRingRowBytes), 16, 0, 0);
   };
   constexpr int kDmaPerChunk = PW;                       // transfers that a wave issues per chunk
-  // Q8: this lane's share of a chunk on its way through registers
+  // the cache's forms: powers of two of K and V of this head (see above), and whether its scales lie too far apart
+  [[maybe_unused]] int k_power = 0, v_power = 0;
+  [[maybe_unused]] bool wide_range = false;
+  [[maybe_unused]] const int64_t scale_row = KV ? (int64_t)bh * scales_blocks(scales) : 0;
+  [[maybe_unused]] HeadScales head_k, head_v;
+  [[maybe_unused]] float first_k = 0.f, first_v = 0.f;   // this lane's block scales (zeros do not count)
+  [[maybe_unused]] auto join_scales = [&]() {
+    head_k.add(first_k); head_v.add(first_v);
+    head_k.join(); head_v.join();
+    k_power = head_k.power(); v_power = head_v.power();
+    wide_range = head_k.wide() || head_v.wide();
+  };
+  // KV = 2: the segment that this wave's next rows begin in (the list goes through the key scales in order); lane k holds
+  // scale k's first token and shift
+  [[maybe_unused]] int seg = 0, my_off = 0, my_shift = 0;
+  if constexpr (KV == 2) {
+    const int i = min(lane, kMaxScales);
+    my_off = scales.off[i]; my_shift = scales.shift[i];
+  }
+  [[maybe_unused]] auto block_of = [&](int tok) -> int {
+    int shift = __builtin_amdgcn_readlane(my_shift, seg);
+    while (seg < gd.k) {
+      const bool beyond = tok >= __builtin_amdgcn_readlane(my_off, seg + 1);
+      if (__builtin_amdgcn_ballot_w64(beyond) == 0) break;
+      ++seg;
+      shift = beyond ? __builtin_amdgcn_readlane(my_shift, seg) : shift;
+    }
+    return (tok + shift) >> 6;
+  };
+  // codes: this lane's share of a chunk on its way through registers
   struct ChunkRegs { u32x4 codes; float2 sz; };
   const bool q8_v = PW == 2 ? lane >= 32 : wave >= 8;     // the lane works on V rows (else K rows)
   const bool q8_active = PW == 2 || lane < 32;
@@ -270,9 +330,13 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c) {
     if (q8_active) {
       tok = checked_index(a.hdr, tok, a.kv_len);
       const unsigned char* base = q8_v ? Vp : Kp;
-      const float2* sz = (q8_v ? a.v_sz : a.k_sz) + (int64_t)(b * a.H + h) * (a.ks[1] / a.ks[2]);
       r.codes = *(const u32x4*)(base + __umul24((unsigned)tok, row_bytes) + 16u * ((unsigned)lane & 3u));
-      r.sz = sz[tok];
+      if constexpr (KV == 2) {
+        r.sz.x = ((q8_v ? scales.v : scales.k) + scale_row)[block_of(tok)];
+      } else {
+        const float2* sz = (q8_v ? a.v_sz : a.k_sz) + (int64_t)(b * a.H + h) * (a.ks[1] / a.ks[2]);
+        r.sz = sz[tok];
+      }
     }
     return r;
   };
@@ -281,6 +345,12 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c) {
     const unsigned slot = (unsigned)((t % kRingChunks) * C + row);
     const unsigned sw = ring_swizzle((unsigned)row), p2 = 2u * ((unsigned)lane & 3u);
     unsigned char* dst = (q8_v ? Vring : Kring) + slot * kRingRowBytes;
+    if constexpr (KV == 2) {
+      const float s = ldexpf(r.sz.x, q8_v ? v_power : k_power);
+      *(f16x8*)(dst + ((p2 ^ sw) << 4)) = codes_to_f16(r.codes[0], r.codes[1], s);
+      *(f16x8*)(dst + (((p2 + 1u) ^ sw) << 4)) = codes_to_f16(r.codes[2], r.codes[3], s);
+      return;
+    }
     bf16x8 lo, hi;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -368,6 +438,11 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c) {
   // The loads go out in the order in which their results are needed: tokens (the transfers of the first three chunks
   // wait for them), step descriptors, Q.  The transfers follow (a load issued behind a chunk is held up until the
   // chunk's data is in), and what needs no memory is formed behind them.
+  if constexpr (KV != 0) {
+    for (int i = 64 + lane; i < scales.n_seen; i += 64) { head_k.add(scales.k[scale_row + i]); head_v.add(scales.v[scale_row + i]); }
+    const int64_t at = scale_row + min(lane, scales.n_seen - 1);
+    first_k = scales.k[at]; first_v = scales.v[at];
+  }
   int tok0 = load_tok(0), tok1 = load_tok(1), tok2 = load_tok(2);
   // Step descriptors for one phase: the first step's is fetched during the phase
   // before (d0), those of the next kLater steps at the start of the phase (dl).
@@ -429,17 +504,18 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c) {
   int t0 = row, t1 = min(1, NC - 1) * C + row, t2 = min(2, NC - 1) * C + row;
   if (!in_prefix) { t0 = tok0; t1 = tok1; t2 = tok2; }   // (waits for the tokens only)
   asm volatile("" : "+v"(t0), "+v"(t1), "+v"(t2));      // (all three formed before the first transfer)
-  if constexpr (Q8) {
+  if constexpr (CODES) {
     // through registers: the three chunks are requested together, converted and written, and
     // the first barrier finds all of them in the ring
     const ChunkRegs c0 = load_chunk(t0), c1 = load_chunk(t1), c2 = load_chunk(t2);
+    if constexpr (KV != 0) join_scales();
     commit_chunk(0, c0); commit_chunk(1, c1); commit_chunk(2, c2);
   } else {
     issue_chunk(0, row_at(t0)); issue_chunk(1, row_at(t1)); issue_chunk(2, row_at(t2));
   }
   __builtin_amdgcn_sched_barrier(0);
 
-  std::conditional_t<WIDE, WidePatchState, PatchState> ps;
+  std::conditional_t<WIDE, WidePatchState<E8>, PatchState> ps;
   [[maybe_unused]] const uint64_t queries = (uint64_t)(unsigned)pw.valid * 0x100000001ull;   // wide: the lanes that hold a query
   [[maybe_unused]] const bool band = (pw.sk_ny & 0xffff) == 0;
   [[maybe_unused]] const float slack = kSlack / c;
@@ -462,11 +538,30 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c) {
     asm volatile("" : "+v"(ones));   // kept in four registers (the compiler would rebuild it in every step)
   }
   // everything older than chunks 1 and 2 is in: Q, the descriptors and tokens, chunk 0 (Q8: all three chunks)
-  if constexpr (Q8) wait_vmcnt<0>(); else wait_vmcnt<2 * kDmaPerChunk>();
+  if constexpr (CODES) wait_vmcnt<0>(); else wait_vmcnt<2 * kDmaPerChunk>();
+  [[maybe_unused]] float c_lane = c;           // KV: softmax scale of this lane's query, its and K's powers of two taken out
+  [[maybe_unused]] int q_power = 0;
+  if constexpr (KV != 0) {
+    float mx = 0.f;
+#pragma unroll
+    for (int t = 0; t < kQPieces; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mx = fmaxf(mx, fmaxf(fabsf(__uint_as_float(q_raw[t][e] << 16)), fabsf(__uint_as_float(q_raw[t][e] & 0xffff0000u))));
+    q_power = power_to_14(fmaxf(mx, other_half(mx)));
+    if constexpr (!CODES) join_scales();
+    if (wide_range) ps.far = queries;
+    c_lane = ldexpf(c, -(q_power + k_power));
+  }
 #pragma unroll
   for (int t = 0; t < kQPieces; ++t) {
-    bf16x8 piece;
-    if constexpr (Q8) {
+    E8 piece;
+    if constexpr (KV != 0) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const unsigned w = q_raw[t][e >> 1];
+        piece[e] = (_Float16)ldexpf(__uint_as_float(e & 1 ? w & 0xffff0000u : w << 16), q_power);
+      }
+    } else if constexpr (Q8) {
       const unsigned w0 = q_raw[t >> 1][2 * (t & 1)], w1 = q_raw[t >> 1][2 * (t & 1) + 1];
 #pragma unroll
       for (int e = 0; e < 8; ++e) piece[e] = (__bf16)fmaf(q_sz.x, (float)(int8_t)(((e < 4 ? w0 : w1) >> (8 * (e & 3))) & 0xffu), q_sz.y);
@@ -477,7 +572,7 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c) {
     else if (t == 0) ps.qb0 = piece;
     else ps.qb1 = piece;
   }
-  if constexpr (Q8) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // (the ring writes above are visible)
+  if constexpr (CODES) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // (the ring writes above are visible)
   else asm volatile("s_barrier" ::: "memory");
   asm volatile("" : : "v"(tok0), "v"(tok1), "v"(tok2));   // (their registers stay theirs until here: no wait before another use)
 
@@ -604,29 +699,42 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c) {
     lds_wait_k(kr[0], kr[1], kr[2], kr[3]);
 #pragma unroll
     for (int t = 0; t < 4; ++t)
-      S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[t]), ps.q[t], S, 0, 0, 0);
+      S = mfma32(__builtin_bit_cast(E8, kr[t]), ps.q[t], S);
     u32x2 va[8];
     lds_read_v_wide<VOFF>(v, x, va);
     __builtin_amdgcn_sched_barrier(0);         // (the reads go out here, not behind the exponentials)
-    bf16x8 pb[2];
+    E8 pb[2];
     float sum;
+    const float cs = KV ? c_lane : c;
     auto exponentials = [&]() {
       sum = ps.L;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
+        if constexpr (KV != 0) {
+          u32x4 two;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) pb[t][e] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(S[8 * t + e], c, ps.negm));
+          for (int e = 0; e < 4; ++e) {
+            const auto h = __builtin_amdgcn_cvt_pkrtz(__builtin_amdgcn_exp2f(__builtin_fmaf(S[8 * t + 2 * e], cs, ps.negm)),
+                                                      __builtin_amdgcn_exp2f(__builtin_fmaf(S[8 * t + 2 * e + 1], cs, ps.negm)));
+            two[e] = __builtin_bit_cast(unsigned, h);
+            sum = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, h), kHalfOnes, sum, false);
+          }
+          pb[t] = __builtin_bit_cast(E8, two);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-          const bf16x2 two = {pb[t][e], pb[t][e + 1]};
-          sum = __builtin_amdgcn_fdot2_f32_bf16(two, kOnes, sum, false);
+          for (int e = 0; e < 8; ++e) pb[t][e] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(S[8 * t + e], cs, ps.negm));
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            const bf16x2 two = {pb[t][e], pb[t][e + 1]};
+            sum = __builtin_amdgcn_fdot2_f32_bf16(two, kOnes, sum, false);
+          }
         }
       }
     };
     exponentials();
-    uint64_t move = __builtin_amdgcn_ballot_w64(sum > kMostSum);
+    uint64_t move = __builtin_amdgcn_ballot_w64(sum > kMost);
     if (__builtin_expect(ps.unset != 0, 0)) {
-      ps.unset = __builtin_amdgcn_ballot_w64(sum + other_half(sum) < kLeastSum) & queries;
+      ps.unset = __builtin_amdgcn_ballot_w64(sum + other_half(sum) < kLeast) & queries;
       move |= ps.unset;
     }
     if (__builtin_expect(move != 0, 0)) {
@@ -635,16 +743,16 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c) {
       for (int e = 1; e < 16; ++e) mx = fmaxf(mx, S[e]);
       mx = fmaxf(mx, other_half(mx));                    // over both lanes of the query
       const float now = sum + other_half(sum), before = ps.L + other_half(ps.L);
-      float to = mx > -INFINITY ? __builtin_fmaf(mx, c, ps.negm) : kFloor;
+      float to = mx > -INFINITY ? __builtin_fmaf(mx, cs, ps.negm) : kFloor;
       if (before > 0.f) to = fmaxf(to, __builtin_amdgcn_logf(before));         // (base 2)
-      const float shift = (now > kMostSum || now < kLeastSum) && to > kFloor ? rintf(to) : 0.f;
+      const float shift = (now > kMost || now < kLeast) && to > kFloor ? rintf(to) : 0.f;
       const float alpha = before > 0.f ? __builtin_amdgcn_exp2f(-shift) : 1.f;
       ps.negm -= shift; ps.L *= alpha;
       ps.far |= is_far(ps.negm);
 #pragma unroll
       for (int e = 0; e < 16; ++e) { ps.O[0][e] *= alpha; ps.O[1][e] *= alpha; }
       exponentials();
-      if (ps.unset) ps.unset = __builtin_amdgcn_ballot_w64(sum + other_half(sum) < kLeastSum) & queries;
+      if (ps.unset) ps.unset = __builtin_amdgcn_ballot_w64(sum + other_half(sum) < kLeast) & queries;
     }
     ps.L = sum;
     lds_wait_v_wide(va);
@@ -653,7 +761,7 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c) {
 #pragma unroll
       for (int dt = 0; dt < 2; ++dt) {
         const uint4 v8 = {va[4 * t + dt].x, va[4 * t + dt].y, va[4 * t + 2 + dt].x, va[4 * t + 2 + dt].y};
-        ps.O[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v8), pb[t], ps.O[dt], 0, 0, 0);
+        ps.O[dt] = mfma32(__builtin_bit_cast(E8, v8), pb[t], ps.O[dt]);
       }
   };
   auto run_step = [&](const Desc cur, int s) {
@@ -682,11 +790,11 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c) {
       d0 = load_desc(min(end, last));
       if constexpr (!FIRST) {
         [[maybe_unused]] unsigned r0 = 0, r1 = 0;
-        if constexpr (Q8) { cr0 = load_chunk(tokn0); cr1 = load_chunk(tokn1); }
+        if constexpr (CODES) { cr0 = load_chunk(tokn0); cr1 = load_chunk(tokn1); }
         else { r0 = row_at(tokn0); r1 = row_at(tokn1); asm volatile("" : "+v"(r0), "+v"(r1)); }   // (formed before the registers are loaded again)
         tokn0 = load_tok(2 * ph + 3); tokn1 = load_tok(2 * ph + 4);
         // the chunks of phase ph + 1, into the slots of chunks 2 ph - 4 and 2 ph - 3
-        if constexpr (!Q8) { issue_chunk(2 * ph + 1, r0); issue_chunk(2 * ph + 2, r1); }
+        if constexpr (!CODES) { issue_chunk(2 * ph + 1, r0); issue_chunk(2 * ph + 2, r1); }
       }
     }
 #pragma unroll
@@ -701,7 +809,7 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c) {
     // for its own), so after the barrier the slots of chunks 2 ph - 3 and 2 ph - 2 are free.
     wait_vmcnt<0>();
     if (!next) return false;
-    if constexpr (Q8 && !FIRST) {
+    if constexpr (CODES && !FIRST) {
       // (their slots held chunks 2 ph - 4 and 2 ph - 3, which nobody has read since the
       // barrier that ended phase ph - 1; the writes are complete before this phase's barrier)
       commit_chunk(2 * ph + 1, cr0); commit_chunk(2 * ph + 2, cr1);
@@ -729,7 +837,9 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c) {
     for (int dt = 0; dt < 2; ++dt)
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
-        const bf16x2 two = {(__bf16)(ps.O[dt][e] * inv), (__bf16)(ps.O[dt][e + 1] * inv)};
+        float x = ps.O[dt][e] * inv, y = ps.O[dt][e + 1] * inv;
+        if constexpr (KV != 0) { x = ldexpf(x, -v_power); y = ldexpf(y, -v_power); }
+        const bf16x2 two = {(__bf16)x, (__bf16)y};
         any = __builtin_amdgcn_fdot2_f32_bf16(two, kOnes, any, false);
         r[dt][e / 2] = __builtin_bit_cast(unsigned, two);
       }
@@ -758,8 +868,8 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c) {
           if (shared) *(u32x4*)(op + (a.B / 2) * a.os[0] + 32 * dt + 16 * j) = piece;
         }
     }
-    attend_rows<Q8>(a, c, b, h, shared, rows_again, qrow, bad_dims,
-                    [&](int row) { return StepKeys(a, a.waves + (size_t)grp_g * kGroupPatches, row); });
+    attend_rows<Q8, KV != 0>(a, c, b, h, shared, rows_again, qrow, bad_dims,
+                             [&](int row) { return StepKeys(a, a.waves + (size_t)grp_g * kGroupPatches, row); }, scales);
   } else {
     if (qrow < 0) return;
     qrow = checked_index(a.hdr, qrow, a.q_len);
@@ -776,11 +886,11 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c) {
   }
 }
 
-litevar_status launch_attn_bf16_pair(const litevar_plan* pl, const AttnArgs& args, hipStream_t st) {
+static litevar_status launch_pair(const litevar_plan* pl, const AttnArgs& args, const KV8Scales* scales, int kv, hipStream_t st) {
   if (pl->waves_per_group != 16 || pl->chunk_keys != kDmaKeys || pl->ring_chunks != kRingChunks)
     return fail(LITEVAR_E_PLAN_CORRUPT, "no 16-patch kernel for chunk=%d ring=%d", pl->chunk_keys, pl->ring_chunks);
   AttnArgs a = args;
-  const int64_t blocks = spread_over_xcds(a, a.n_groups, a.k_sz ? 72 : 128);
+  const int64_t blocks = spread_over_xcds(a, a.n_groups, a.k_sz ? 72 : kv == 2 ? 64 : 128);
   if (blocks > 0x7fffffff) return fail(LITEVAR_E_UNSUPPORTED, "grid too large");
   // Sixteen waves with a 16-query patch each where the plan asks for them, or can have no wide patches.  They are nowhere
   // quicker, on a CU of their own either: 256 queries on 680 keys, 60 / 240 pairs 14.0 / 17.0 us, wide 13.4 / 16.4; 169
@@ -792,6 +902,7 @@ litevar_status launch_attn_bf16_pair(const litevar_plan* pl, const AttnArgs& arg
   if ((has_wide && pl->patches_per_wave == 1) || pl->off[kSecStepAddr] - pl->off[kSecUnion] != (uint64_t)pl->n_union_keys * sizeof(int32_t))
     return fail(LITEVAR_E_PLAN_CORRUPT, "the plan's sections are not those of this library");
   const int pw = has_wide ? 2 : 1;
+  if (kv != 0 && pw != 2) return fail(LITEVAR_E_UNSUPPORTED, "the plan has no wide patches");
   WideArgs w{};
   w.waves = a.waves + groups * 16;
   // all workgroups are resident at once (two per CU): see later_arrival
@@ -807,11 +918,21 @@ litevar_status launch_attn_bf16_pair(const litevar_plan* pl, const AttnArgs& arg
   const dim3 wg(kGroupPatches / pw * 64);
   return launch_in_parts(blocks, (int)wg.x, "bf16 attention launch", [&](int64_t first, unsigned n) {
     a.first_block = (uint32_t)first;
-    if (pw == 1 && q8) hipLaunchKernelGGL((k_attn_bf16_pair<1, true>), dim3(n), wg, 0, st, a, w, c);
-    else if (pw == 1) hipLaunchKernelGGL((k_attn_bf16_pair<1, false>), dim3(n), wg, 0, st, a, w, c);
-    else if (q8) hipLaunchKernelGGL((k_attn_bf16_pair<2, true>), dim3(n), wg, 0, st, a, w, c);
-    else hipLaunchKernelGGL((k_attn_bf16_pair<2, false>), dim3(n), wg, 0, st, a, w, c);
+    if (kv == 2) hipLaunchKernelGGL((k_attn_bf16_pair<2, false, 2>), dim3(n), wg, 0, st, a, w, c, *scales);
+    else if (kv == 1) hipLaunchKernelGGL((k_attn_bf16_pair<2, false, 1>), dim3(n), wg, 0, st, a, w, c, *scales);
+    else if (pw == 1 && q8) hipLaunchKernelGGL((k_attn_bf16_pair<1, true>), dim3(n), wg, 0, st, a, w, c, NoScales{});
+    else if (pw == 1) hipLaunchKernelGGL((k_attn_bf16_pair<1, false>), dim3(n), wg, 0, st, a, w, c, NoScales{});
+    else if (q8) hipLaunchKernelGGL((k_attn_bf16_pair<2, true>), dim3(n), wg, 0, st, a, w, c, NoScales{});
+    else hipLaunchKernelGGL((k_attn_bf16_pair<2, false>), dim3(n), wg, 0, st, a, w, c, NoScales{});
   });
+}
+
+litevar_status launch_attn_bf16_pair(const litevar_plan* pl, const AttnArgs& a, hipStream_t st) {
+  return launch_pair(pl, a, nullptr, 0, st);
+}
+
+litevar_status launch_attn_kv8_pair(const litevar_plan* pl, const AttnArgs& a, const KV8Scales& scales, bool in_kernel, hipStream_t st) {
+  return launch_pair(pl, a, &scales, in_kernel ? 2 : 1, st);
 }
 
 }  // namespace lv

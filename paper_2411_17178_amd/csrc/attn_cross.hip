@@ -35,6 +35,7 @@ struct CrossArgs {
   int scale_blocks;                            // of a (batch, kv head)
   uint32_t q_magic, tiles_magic, hkv_magic, parts_magic, pairs_magic;   // see divmod_by
   uint32_t first_block;
+  int groups, by_xcd; uint32_t groups_magic;   // k_cross_tiles: workgroups of a pair, how they are laid out
   float* part_o; float2* part_ml;              // [item][32][64] and [item][32] (largest score, sum), item = workgroup
 };
 
@@ -355,18 +356,25 @@ __device__ inline void row_again(const CrossArgs& a, float c, int b, int j, int 
 // Codes: a chunk is a block, its K scale joins the softmax scale.  Its V scale, relative to the largest of the
 // keys that count, is added to the exponent, which costs nothing per score; the chunk's part of the row sum is divided by it
 // again.  (Relative V scales are taken as at least 2^-96, so that no probability that counts is flushed to zero.)
-template <int NWV, int BUFS, int KIND>
-__global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(NWV == 4 && BUFS == 3 ? 3 : 4, NWV == 4 && BUFS == 3 ? 3 : 4)))
+template <int NWV, int KIND>
+__global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(NWV == 4 ? 3 : 4, NWV == 4 ? 3 : 4)))
 void k_cross_tiles(CrossArgs a, float c) {
   constexpr bool CODES = KIND == kCodes;
   constexpr int kRowsPerWave = kBlock / NWV, kTransfers = kRowsPerWave / 8, kBuf = 2 * kBlock * kRow;
-  __shared__ __align__(1024) unsigned char smem[BUFS * kBuf];
+  __shared__ __align__(1024) unsigned char smem[3 * kBuf];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int n = lane & 31, hh = lane >> 5;
-  // all (batch, kv head) pairs of one tile next to each other: workgroup i runs on XCD i % 8, so the tiles of a pair share
-  // an L2 where there are eight pairs to an eighth, and few pairs still use all XCDs
+  // Workgroup i runs on XCD i % 8, each with an L2 of its own: the tiles of a pair follow one another on one XCD, or, with
+  // few pairs, all pairs of one tile follow one another, which uses all XCDs.
   int tile, bj, b, j;
-  divmod_by(a.first_block + blockIdx.x, (uint32_t)(a.B * a.Hkv), a.pairs_magic, tile, bj);
+  const uint32_t block = a.first_block + blockIdx.x;
+  if (a.by_xcd) {
+    divmod_by(block >> 3, (uint32_t)a.groups, a.groups_magic, bj, tile);
+    bj = 8 * bj + (int)(block & 7);
+    if (bj >= a.B * a.Hkv) return;
+  } else {
+    divmod_by(block, (uint32_t)(a.B * a.Hkv), a.pairs_magic, tile, bj);
+  }
   divmod_by((uint32_t)bj, (uint32_t)a.Hkv, a.hkv_magic, b, j);
   const int n_keys = keys_of(a, b);
   const int row0 = (tile * NWV + wave) * kRows;
@@ -545,7 +553,7 @@ void k_cross_tiles(CrossArgs a, float c) {
     // blocks the next chunk is made sure of and the one after it requested, for the buffer that every wave has read to
     // its end by then.
     auto one = [&](int chunk, auto which) -> bool {
-      constexpr int p = decltype(which)::value, AT = p * kBuf, NEXT = (p + 1) % BUFS * kBuf;
+      constexpr int p = decltype(which)::value, AT = p * kBuf, NEXT = (p + 1) % 3 * kBuf;
       const int key0 = chunk * kBlock;
       const bool more = chunk + 1 < n_chunks, second = key0 + 32 < n_keys;
       float ks = 1.f, lv = 0.f, iv = 1.f;
@@ -570,14 +578,14 @@ void k_cross_tiles(CrossArgs a, float c) {
       }
       if (more) {
         if constexpr (CODES) {
-          commit_chunk((p + 1) % BUFS);
+          commit_chunk((p + 1) % 3);
           if (chunk + 2 < n_chunks) load_chunk(chunk + 2);
           load_scales(chunk + 1);
           asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         } else {
           wait_vmcnt<0>();
           asm volatile("s_barrier" ::: "memory");
-          if (BUFS == 3 && chunk + 2 < n_chunks) issue_chunk(chunk + 2, (p + 2) % BUFS);
+          if (chunk + 2 < n_chunks) issue_chunk(chunk + 2, (p + 2) % 3);
         }
       }
       if (working && second) {
@@ -591,18 +599,12 @@ void k_cross_tiles(CrossArgs a, float c) {
         __builtin_amdgcn_sched_barrier(0);
         absorb(S1, va, key0 + 32, ks, lv, iv);
       }
-      if (BUFS == 2 && chunk + 2 < n_chunks) {
-        asm volatile("s_barrier" ::: "memory");
-        issue_chunk(chunk + 2, p);
-      }
       return more;
     };
-    for (int chunk = 0;; chunk += BUFS) {
+    for (int chunk = 0;; chunk += 3) {
       if (!one(chunk, std::integral_constant<int, 0>{})) break;
       if (!one(chunk + 1, std::integral_constant<int, 1>{})) break;
-      if constexpr (BUFS == 3) {
-        if (!one(chunk + 2, std::integral_constant<int, 2>{})) break;
-      }
+      if (!one(chunk + 2, std::integral_constant<int, 2>{})) break;
     }
   }
 
@@ -702,11 +704,16 @@ template <int KIND> litevar_status launch(CrossArgs& a, float c, hipStream_t st)
   if constexpr (KIND != kF32) {
     // (64 rows of K or V span less than 4 GiB, see issue_chunk)
     if (a.parts == 1 && a.tiles > 1 && a.ks[2] < (1 << 24)) {
-      const int nwv = KIND != kCodes && a.tiles > 4 ? 8 : 4;
-      return launch_in_parts((int64_t)a.B * a.Hkv * ((a.tiles + nwv - 1) / nwv), nwv * 64, "cross attention launch", [&](int64_t first, unsigned n) {
+      const int nwv = a.tiles > 4 ? 8 : 4;
+      const int64_t pairs = (int64_t)a.B * a.Hkv;
+      a.groups = (a.tiles + nwv - 1) / nwv; a.groups_magic = magic_of(a.groups);
+      a.by_xcd = 9 * pairs >= 8 * ((pairs + 7) / 8 * 8);       // (288 pairs of 2240 rows: 93.0 us pair by pair in turn, 91.7 so)
+      const int64_t blocks = (a.by_xcd ? (pairs + 7) / 8 * 8 : pairs) * a.groups;
+      if (blocks > 0x7fffffff) return fail(LITEVAR_E_UNSUPPORTED, "grid too large");
+      return launch_in_parts(blocks, nwv * 64, "cross attention launch", [&](int64_t first, unsigned n) {
         a.first_block = (uint32_t)first;
-        if (nwv == 8) hipLaunchKernelGGL((k_cross_tiles<8, 3, kBf16>), dim3(n), dim3(512), 0, st, a, c);
-        else hipLaunchKernelGGL((k_cross_tiles<4, 3, KIND>), dim3(n), dim3(256), 0, st, a, c);
+        if (nwv == 8) hipLaunchKernelGGL((k_cross_tiles<8, KIND>), dim3(n), dim3(512), 0, st, a, c);
+        else hipLaunchKernelGGL((k_cross_tiles<4, KIND>), dim3(n), dim3(256), 0, st, a, c);
       });
     }
   }

@@ -110,10 +110,20 @@ litevar_status make_attn_args(const litevar_plan* plan, int32_t B, int32_t H, in
 // (t + shift[j]) / 64, segment j begins at token off[j].
 struct KV8Scales {
   const float* k; const float* v;              // [B][H][n_blocks]
-  int n_blocks;
+  const int8_t* k8; const int8_t* v8;          // [B][H][kv_len][64]
+  int n_blocks, n_seen;                        // in all, and of the scales that the plan's queries see
   int off[kMaxScales + 1], shift[kMaxScales + 1];
+#ifdef __HIPCC__
+  __device__ int block_of(int tok, int n_scales) const {
+    int s = 0;
+    for (int j = 1; j < n_scales; ++j) s = tok >= off[j] ? shift[j] : s;
+    return (tok + s) >> 6;
+  }
+#endif
 };
 
+// in_kernel: the codes are converted on their way into LDS; else a.k and a.v are copies that launch_kv8_copy made
+litevar_status launch_attn_kv8_pair(const litevar_plan* pl, const AttnArgs& a, const KV8Scales& scales, bool in_kernel, hipStream_t st);
 litevar_status launch_attn_kv8(const litevar_plan* pl, const AttnArgs& a, const KV8Scales& scales, hipStream_t st);
 litevar_status launch_attn_f32(const litevar_plan* pl, const AttnArgs& a, hipStream_t st);
 litevar_status launch_attn_bf16(const litevar_plan* pl, const AttnArgs& a, hipStream_t st);

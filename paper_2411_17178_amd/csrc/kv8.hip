@@ -34,7 +34,7 @@ struct StoreArgs {
 struct LoadArgs {
   Blocks w;
   const int8_t* codes[2]; const float* scale[2];
-  __bf16* out[2];
+  unsigned short* out[2];
 };
 
 struct Block { int b, bh, h, index, token, rows; };
@@ -133,27 +133,38 @@ __global__ __launch_bounds__(kWaves * 64) void k_kv8_store(StoreArgs a) {
   if (lane == 0) (tensor ? a.scale[1] : a.scale[0])[(int64_t)k.bh * a.w.total_blocks + k.index] = s;
 }
 
-// Codes -> bf16 rows [B][H][len][64]; a wave per block and tensor.
+// Codes -> rows [B][H][len][64] of bf16, or of f16 times the head's power of two (see HeadScales; every wave forms it
+// from the scales of all visited blocks); a wave per block and tensor.
+template <bool F16>
 __global__ __launch_bounds__(kWaves * 64) void k_kv8_load(LoadArgs a) {
   int tensor;
   Block k;
   if (!my_block(a.w, tensor, k)) return;
   const int lane = threadIdx.x & 63, row8 = lane >> 3, part = lane & 7;
-  const float s = (tensor ? a.scale[1] : a.scale[0])[(int64_t)k.bh * a.w.total_blocks + k.index];
+  const float* scales = (tensor ? a.scale[1] : a.scale[0]) + (int64_t)k.bh * a.w.total_blocks;
   const int64_t at = ((int64_t)k.bh * a.w.len + k.token) * 64 + 8 * part;
   const int8_t* codes = (tensor ? a.codes[1] : a.codes[0]) + at;
-  __bf16* out = (tensor ? a.out[1] : a.out[0]) + at;
+  unsigned short* out = (tensor ? a.out[1] : a.out[0]) + at;
   uint2 c[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     if (8 * i < k.rows) c[i] = *(const uint2*)(codes + min(8 * i + row8, k.rows - 1) * 64);
+  float s = scales[k.index];
+  if constexpr (F16) {
+    HeadScales head;
+    for (int i = lane; i < a.w.n_blocks; i += 64) head.add(scales[a.w.first[0] + i]);
+    head.join();
+    s = ldexpf(s, head.power());
+  }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     if (8 * i >= k.rows) break;
-    bf16x8 r;
+    using T = std::conditional_t<F16, _Float16, __bf16>;
+    typedef __attribute__((ext_vector_type(8))) T T8;
+    T8 r;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = (__bf16)(s * (float)(int8_t)(((e < 4 ? c[i].x : c[i].y) >> (8 * (e & 3))) & 0xffu));
-    if (8 * i + row8 < k.rows) *(bf16x8*)(out + (8 * i + row8) * 64) = r;
+    for (int e = 0; e < 8; ++e) r[e] = (T)(s * (float)(int8_t)(((e < 4 ? c[i].x : c[i].y) >> (8 * (e & 3))) & 0xffu));
+    if (8 * i + row8 < k.rows) *(T8*)(out + (8 * i + row8) * 64) = r;
   }
 }
 
@@ -202,6 +213,16 @@ litevar_status launch_blocks(Blocks& w, const char* what, Launch launch) {
     w.first_block = (uint32_t)first;
     launch(n);
   });
+}
+
+// How a plan's cache is read.  Plans whose bf16 calls run 32 queries per wave do so here too: with the codes converted in
+// the attention kernel, once per group that streams a row, or from a copy that is converted once; plans of smaller groups,
+// and handles that ask for sixteen waves, gather codes step by step.
+enum Route { kGather, kInKernel, kCopy };
+Route route_of(const litevar_plan* plan) {
+  if (plan->waves_per_group != 16 || plan->patches_per_wave == 1 || (int64_t)plan->kv_len * 128 >= ((int64_t)1 << 31)) return kGather;
+  const int64_t streamed = plan->n_union_keys / (plan->n_head_groups > 0 ? plan->n_head_groups : 1);
+  return 4 * streamed <= 5 * (2 * (int64_t)plan->kv_len) ? kInKernel : kCopy;
 }
 
 // (the stride of an axis with one entry is never used, and is what it is)
@@ -264,16 +285,16 @@ litevar_status litevar_kv8_load(const int32_t* segments, int32_t n_segments, int
     return fail(LITEVAR_E_INVALID_ARG, "rows and codes must be 16-byte aligned");
   if (((uintptr_t)d_k_scale | (uintptr_t)d_v_scale) & 3) return fail(LITEVAR_E_INVALID_ARG, "scales must be 4-byte aligned");
   a.codes[0] = d_k8; a.codes[1] = d_v8; a.scale[0] = d_k_scale; a.scale[1] = d_v_scale;
-  a.out[0] = (__bf16*)d_k_bf16; a.out[1] = (__bf16*)d_v_bf16;
+  a.out[0] = (unsigned short*)d_k_bf16; a.out[1] = (unsigned short*)d_v_bf16;
   return launch_blocks(a.w, "8-bit cache load", [&](unsigned n_wg) {
-    hipLaunchKernelGGL(k_kv8_load, dim3(n_wg), dim3(kWaves * 64), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL(k_kv8_load<false>, dim3(n_wg), dim3(kWaves * 64), 0, (hipStream_t)stream, a);
   });
 }
 
 litevar_status litevar_windowed_attn_kv8_workspace_bytes(const litevar_plan* plan, int32_t B, int32_t H, size_t* out_bytes) {
   if (!plan || !out_bytes) return fail(LITEVAR_E_INVALID_ARG, "plan or out_bytes is NULL");
   if (B < 1 || H < 1) return fail(LITEVAR_E_INVALID_ARG, "B and H must be positive");
-  *out_bytes = 0;
+  *out_bytes = route_of(plan) == kCopy ? (size_t)B * H * 2 * (size_t)plan->kv_len * 64 * 2 : 0;
   return LITEVAR_OK;
 }
 
@@ -307,7 +328,22 @@ litevar_status litevar_windowed_attn_kv8_fwd(const litevar_plan* plan, const voi
     off += n; first += (n + kBlock - 1) / kBlock;
   }
   scales.n_blocks = first;
-  return launch_attn_kv8(plan, a, scales, (hipStream_t)stream);
+  scales.n_seen = (scales.shift[plan->q_scale_end] + scales.off[plan->q_scale_end]) / kBlock;
+  scales.k8 = d_k8; scales.v8 = d_v8;
+  const Route route = route_of(plan);
+  if (route == kGather) return launch_attn_kv8(plan, a, scales, (hipStream_t)stream);
+  if (route == kInKernel) return launch_attn_kv8_pair(plan, a, scales, true, (hipStream_t)stream);
+  int32_t seg[kMaxScales];
+  for (int k = 0; k < plan->n_scales; ++k) seg[k] = plan->scales[k] * plan->scales[k];
+  LoadArgs copy{};
+  if (litevar_status s = make_blocks(seg, plan->n_scales, 0, plan->q_scale_end, B, H, copy.w)) return s;
+  copy.codes[0] = d_k8; copy.codes[1] = d_v8; copy.scale[0] = d_k_scale; copy.scale[1] = d_v_scale;
+  copy.out[0] = (unsigned short*)d_workspace; copy.out[1] = copy.out[0] + (int64_t)B * H * plan->kv_len * 64;
+  if (litevar_status s = launch_blocks(copy.w, "8-bit cache copy", [&](unsigned n_wg) {
+        hipLaunchKernelGGL(k_kv8_load<true>, dim3(n_wg), dim3(kWaves * 64), 0, (hipStream_t)stream, copy);
+      })) return s;
+  a.k = copy.out[0]; a.v = copy.out[1];
+  return launch_attn_kv8_pair(plan, a, scales, false, (hipStream_t)stream);
 }
 
 }  // extern "C"

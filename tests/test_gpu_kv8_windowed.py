@@ -1,8 +1,12 @@
 """Windowed attention on the 8-bit cache against the formula in 64 bits on the cache's own values.
 
 Tolerance, element by element (A = sum of weights x |v|, S = the row's largest sum of |q_d k_d| x sm_scale, U = half a
-step of bf16): V rounded, U A; probabilities rounded, 2 U A; output rounded, U A; K rounded, which moves a score by
-U S at most and so a weight by the factor exp(2 U S): (exp(2 U S) - 1) 2 A.  Sums in 32 bits: below U A / 8."""
+step of bf16): probabilities rounded, or their products with the V scales, 2 U A; output rounded, U A; V rounded to f16,
+2^-12 A; K rounded to f16, which moves a score by 2^-12 S at most and so a weight by the factor exp(2^-11 S):
+(exp(2^-11 S) - 1) 2 A.  Sums in 32 bits: below U A / 8.  Probabilities in f16 have an absolute floor as well: their last bit is 2^-24 below 2^-14, and a row's sum is at least
+2^-3 (it starts at a reference of 0, and a step that leaves the sum below 2^-3 is formed again under a reference that
+makes its largest probability at least 2^-0.5), so a weight is off by 2^-21 at most; over n kept keys with |v| <= V the
+result by 2^-21 (n V + n |out|) <= 2^-20 n V."""
 import pytest
 import torch
 
@@ -21,8 +25,8 @@ def lv():
     return m
 
 
-def _tolerance(A, S):
-    return (4.125 * plain.U + 2 * torch.expm1(2 * plain.U * S)) * A
+def _tolerance(A, S, floor):
+    return (3.25 * plain.U + 2 * torch.expm1(2.0 ** -11 * S)) * A + 2.0 ** -20 * floor
 
 
 def _cache(lv, scales, B, H, seed, seen=None):
@@ -44,7 +48,9 @@ def _reference(cache, q, mask, sm=SM):
     used = mask.any(-2 if mask.dim() == 2 else 1)                            # tokens that some query keeps
     used = used.view(1, -1, mask.shape[-1], 1)
     zero = torch.zeros((), dtype=torch.float64, device="cuda")
-    return plain.attention(q, torch.where(used, kd, zero), torch.where(used, vd, zero), mask, sm)
+    kd, vd = torch.where(used, kd, zero), torch.where(used, vd, zero)
+    largest = torch.where(mask, vd.abs().amax(-1)[:, :, None], zero).amax(-1, keepdim=True)   # |v| of a row's kept keys
+    return (*plain.attention(q, kd, vd, mask, sm), mask.sum(-1)[..., None] * largest)
 
 
 CASES = [  # scales, query scales, radius, sink scales, mask mode, batch, heads, plan options
@@ -68,8 +74,8 @@ def test_windowed_attention_on_the_cache(lv, case):
     q = torch.randn(B, H, plan.q_len, 64, generator=g, device="cuda").to(torch.bfloat16)
     out = lv.litevar_windowed_attn_kv8_fwd(plan, q, cache, SM)
     mask = lv.litevar_mask_export_dense(plan)[0].bool()
-    want, A, S = _reference(cache, q, mask)
-    plain.assert_close(out, want, _tolerance(A, S))
+    want, A, S, floor = _reference(cache, q, mask)
+    plain.assert_close(out, want, _tolerance(A, S, floor))
     lv.litevar_plan_check(plan)
 
 
@@ -82,8 +88,8 @@ def test_one_radius_table_per_head(lv):
         q = torch.randn(B, H, plan.q_len, 64, device="cuda").to(torch.bfloat16)
         out = lv.litevar_windowed_attn_kv8_fwd(plan, q, cache, SM)
         mask = torch.stack([lv.litevar_mask_export_dense(plan, head=h)[0].bool() for h in range(H)])
-        want, A, S = _reference(cache, q, mask)
-        plain.assert_close(out, want, _tolerance(A, S))
+        want, A, S, floor = _reference(cache, q, mask)
+        plain.assert_close(out, want, _tolerance(A, S, floor))
 
 
 @pytest.mark.parametrize("waves", [0, 16])
@@ -117,8 +123,8 @@ def test_values_that_are_not_finite_stay_in_their_rows(lv):
         lo = cache.offsets[9] + 64
         hit = mask[:, lo:lo + 64].any(-1)
         clean = _cache(lv, VAR256, B, H, 5)
-        want, A, S = _reference(clean, q, mask)
-        tol = _tolerance(A, S)
+        want, A, S, floor = _reference(clean, q, mask)
+        tol = _tolerance(A, S, floor)
         plain.assert_close(out[:, :1], want[:, :1], tol[:, :1])
         plain.assert_close(out[:, 1, ~hit], want[:, 1, ~hit], tol[:, 1, ~hit])
         assert not bool(torch.isfinite(out[:, 1, hit]).all(-1).any())
@@ -152,8 +158,67 @@ def test_whole_generation_with_graph(lv):
         out.fill_(float("nan"))
         graph.replay()
         torch.cuda.synchronize()
-        want, A, S = _reference(cache, q, mask)
-        plain.assert_close(out, want, _tolerance(A, S))
+        want, A, S, floor = _reference(cache, q, mask)
+        plain.assert_close(out, want, _tolerance(A, S, floor))
         replayed = out.clone()
         steps()
         assert torch.equal(out, replayed)
+
+
+ROUTES = [((9, 10), 0), (None, 16), (None, 4), ((9, 10), 8)]     # converted in the kernel, through a copy, gathered, gathered
+
+
+@pytest.mark.parametrize("route", ROUTES, ids=str)
+def test_block_scales_far_apart(lv, route):
+    """K or V blocks 2^-30, 2^-70 and 2^60 times as large as the others, or of zeros: every value at its own size."""
+    q_scales, waves = route
+    B, H = 1, 6
+    plan = lv.litevar_mask_build(VAR256, 2, None, 0, q_scales, waves_per_group=waves)
+    seg = [s * s for s in VAR256]
+    cache = lv.litevar_kv8_cache(seg, B, H)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    k, v = (torch.randn(B, H, 680, 64, generator=g, device="cuda") for _ in range(2))
+    lo = cache.offsets[9]
+    v[:, 0, lo:lo + 64] *= 2.0 ** -30
+    v[:, 1, :lo] *= 2.0 ** -70
+    k[:, 2, lo + 64:lo + 128] *= 2.0 ** -30
+    k[:, 3, lo:] = 0
+    v[:, 4, lo + 64:] = 0
+    v[:, 5, lo:lo + 64] *= 2.0 ** 60
+    lv.litevar_kv8_store(cache, k, v)
+    q = torch.randn(B, H, plan.q_len, 64, generator=g, device="cuda").to(torch.bfloat16)
+    out = lv.litevar_windowed_attn_kv8_fwd(plan, q, cache, SM)
+    want, A, S, floor = _reference(cache, q, lv.litevar_mask_export_dense(plan)[0].bool())
+    plain.assert_close(out, want, _tolerance(A, S, floor))
+
+
+@pytest.mark.parametrize("route", ROUTES, ids=str)
+@pytest.mark.parametrize("shift,spread,size", [(0.0, 0.0, 1.0), (0.0, 6.0, 1.0), (-24.0, 6.0, 1.0), (40.0, 1.0, 1e4), (0.0, 30.0, 1e-4), (-300.0, 1.0, 1.0)])
+def test_distributions_of_scores(lv, route, shift, spread, size):
+    """Flat, peaked, low and high scores, V of many sizes: the weights keep their relative precision."""
+    q_scales, waves = route
+    B, H = 1, 3
+    plan = lv.litevar_mask_build(VAR256, 3, None, 0, q_scales, waves_per_group=waves)
+    cache = lv.litevar_kv8_cache([s * s for s in VAR256], B, H)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    k, v = (torch.randn(B, H, 680, 64, generator=g, device="cuda") for _ in range(2))
+    q = torch.randn(B, H, plan.q_len, 64, generator=g, device="cuda") * spread
+    q[..., 0] = 1.0
+    k[..., 0] = shift / SM                                # (a score's mean; the codes keep it to half a step)
+    lv.litevar_kv8_store(cache, k, v * size)
+    q = q.to(torch.bfloat16)
+    out = lv.litevar_windowed_attn_kv8_fwd(plan, q, cache, SM)
+    want, A, S, floor = _reference(cache, q, lv.litevar_mask_export_dense(plan)[0].bool())
+    plain.assert_close(out, want, _tolerance(A, S, floor))
+
+
+@pytest.mark.parametrize("sm", [1e-30, 1e-6, 1.0, 1e4])
+def test_softmax_scales(lv, sm):
+    B, H = 1, 2
+    for q_scales, waves in ROUTES:
+        plan = lv.litevar_mask_build(VAR256, 3, None, 0, q_scales, waves_per_group=waves)
+        cache = _cache(lv, VAR256, B, H, 8)
+        q = (torch.randn(B, H, plan.q_len, 64, device="cuda") * min(1.0, 1.0 / sm)).to(torch.bfloat16)
+        out = lv.litevar_windowed_attn_kv8_fwd(plan, q, cache, sm)
+        want, A, S, floor = _reference(cache, q, lv.litevar_mask_export_dense(plan)[0].bool(), sm)
+        plain.assert_close(out, want, _tolerance(A, S, floor))
