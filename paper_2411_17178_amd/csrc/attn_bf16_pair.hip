@@ -214,7 +214,8 @@ struct StepKeys {
 // relative to its norm, by 0.0018 so; the store's own rounding is 0.0017.  Heads whose block scales differ by more than 2^20
 // would lose bits of the smaller blocks: all their rows are formed again from the codes.
 //   KV = 1: K and V are copies in f16 (k_kv8_copy), which come by LDS-DMA.
-//   KV = 2: the codes are converted on their way into LDS, as with Q8.
+//   KV = 2: LDS-DMA takes the codes to the ring and they are converted in place at the end of the phase (no registers are
+//     held in between; as with Q8, through registers and with three chunks converted before the first barrier, @Q8@).
 template <int PW, bool Q8, int KV = 0>
 __global__ __launch_bounds__((kGroupPatches / PW) * 64) __attribute__((amdgpu_waves_per_eu(4, 4)))
 void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV != 0, KV8Scales, NoScales> scales) {
@@ -274,7 +275,7 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
   const unsigned row_bytes = (unsigned)a.ks[2] * kKvElem; // a (batch, head) slab spans < 2 GiB (checked by the API)
   const int32_t* utok = a.union_tok + gd.union_base;
   // bf16: eight lanes per 128-byte row; codes: four lanes per 64-byte row
-  const int row = CODES ? 8 * (wave & 7) + ((lane >> 2) & 7) : 8 * (wave & 7) + (lane >> 3);
+  const int row = KV == 2 ? 16 * (wave & 3) + (lane >> 2) : CODES ? 8 * (wave & 7) + ((lane >> 2) & 7) : 8 * (wave & 7) + (lane >> 3);
   // A lane's row of chunk t goes to slot (t % 5) * 64 + row.  Chunks start at multiples of 64
   // slots, so the slot's swizzle -- and with it the 16-byte piece of the source row that
   // this lane fetches -- does not depend on t.
@@ -300,7 +301,7 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
   [[maybe_unused]] auto join_scales = [&]() {
     head_k.add(first_k); head_v.add(first_v);
     head_k.join(); head_v.join();
-    k_power = head_k.power(); v_power = head_v.power();
+    k_power = __builtin_amdgcn_readfirstlane(head_k.power()); v_power = __builtin_amdgcn_readfirstlane(head_v.power());
     wide_range = head_k.wide() || head_v.wide();
   };
   // KV = 2: the segment that this wave's next rows begin in (the list goes through the key scales in order); lane k holds
@@ -320,7 +321,33 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
     }
     return (tok + shift) >> 6;
   };
-  // codes: this lane's share of a chunk on its way through registers
+  // KV = 2: waves 0-3 bring K rows, waves 4-7 V rows, sixteen of a chunk each (what a wave needs of K or V is then
+  // the same for its lanes).  One transfer takes their codes to where the rows will be (the first half of 2 KiB, nobody
+  // else's); convert_chunk reads them back and writes the rows.
+  [[maybe_unused]] const bool v_rows = wave >= 4;
+  [[maybe_unused]] auto scale_of = [&](int tok) -> float {         // of this lane's row
+    if constexpr (KV == 2) return ((v_rows ? scales.v : scales.k) + scale_row)[block_of(checked_index(a.hdr, tok, a.kv_len))];
+    return 0.f;
+  };
+  [[maybe_unused]] unsigned char* const my_ring = (v_rows ? Vring : Kring) + 16 * (wave & 3) * kRingRowBytes;
+  [[maybe_unused]] auto issue_codes = [&](int t, int tok) {
+    const unsigned at = __umul24((unsigned)checked_index(a.hdr, tok, a.kv_len), 64u) + 16u * ((unsigned)lane & 3u);
+    __builtin_amdgcn_global_load_lds((global_void*)((v_rows ? Vp : Kp) + at), (lds_void*)(my_ring + (t % kRingChunks) * C * kRingRowBytes), 16, 0, 0);
+  };
+  [[maybe_unused]] auto convert_chunk = [&](int t, float scale) {
+    const unsigned sw = ring_swizzle((unsigned)row), p2 = 2u * ((unsigned)lane & 3u);
+    const unsigned base = lds_addr(my_ring + (t % kRingChunks) * C * kRingRowBytes);
+    const unsigned codes_at = base + 16u * (unsigned)lane, to = base + (unsigned)(lane >> 2) * kRingRowBytes;
+    u32x4 w;
+    asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=v"(w) : "v"(codes_at) : "memory");
+    const float s = ldexpf(scale, v_rows ? v_power : k_power);
+    const unsigned w0 = w[0], w1 = w[1], w2 = w[2], w3 = w[3];
+    const u32x4 lo = __builtin_bit_cast(u32x4, codes_to_f16(w0, w1, s)), hi = __builtin_bit_cast(u32x4, codes_to_f16(w2, w3, s));
+    asm volatile("ds_write_b128 %0, %2\n\tds_write_b128 %1, %3"
+                 : : "v"(to + ((p2 ^ sw) << 4)), "v"(to + (((p2 + 1u) ^ sw) << 4)), "v"(lo), "v"(hi) : "memory");
+  };
+  [[maybe_unused]] float scale1 = 0.f, scale2 = 0.f;     // of the two chunks that are on their way
+  // Q8: this lane's share of a chunk on its way through registers
   struct ChunkRegs { u32x4 codes; float2 sz; };
   const bool q8_v = PW == 2 ? lane >= 32 : wave >= 8;     // the lane works on V rows (else K rows)
   const bool q8_active = PW == 2 || lane < 32;
@@ -331,12 +358,8 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
       tok = checked_index(a.hdr, tok, a.kv_len);
       const unsigned char* base = q8_v ? Vp : Kp;
       r.codes = *(const u32x4*)(base + __umul24((unsigned)tok, row_bytes) + 16u * ((unsigned)lane & 3u));
-      if constexpr (KV == 2) {
-        r.sz.x = ((q8_v ? scales.v : scales.k) + scale_row)[block_of(tok)];
-      } else {
-        const float2* sz = (q8_v ? a.v_sz : a.k_sz) + (int64_t)(b * a.H + h) * (a.ks[1] / a.ks[2]);
-        r.sz = sz[tok];
-      }
+      const float2* sz = (q8_v ? a.v_sz : a.k_sz) + (int64_t)(b * a.H + h) * (a.ks[1] / a.ks[2]);
+      r.sz = sz[tok];
     }
     return r;
   };
@@ -345,12 +368,6 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
     const unsigned slot = (unsigned)((t % kRingChunks) * C + row);
     const unsigned sw = ring_swizzle((unsigned)row), p2 = 2u * ((unsigned)lane & 3u);
     unsigned char* dst = (q8_v ? Vring : Kring) + slot * kRingRowBytes;
-    if constexpr (KV == 2) {
-      const float s = ldexpf(r.sz.x, q8_v ? v_power : k_power);
-      *(f16x8*)(dst + ((p2 ^ sw) << 4)) = codes_to_f16(r.codes[0], r.codes[1], s);
-      *(f16x8*)(dst + (((p2 + 1u) ^ sw) << 4)) = codes_to_f16(r.codes[2], r.codes[3], s);
-      return;
-    }
     bf16x8 lo, hi;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -504,11 +521,14 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
   int t0 = row, t1 = min(1, NC - 1) * C + row, t2 = min(2, NC - 1) * C + row;
   if (!in_prefix) { t0 = tok0; t1 = tok1; t2 = tok2; }   // (waits for the tokens only)
   asm volatile("" : "+v"(t0), "+v"(t1), "+v"(t2));      // (all three formed before the first transfer)
-  if constexpr (CODES) {
+  [[maybe_unused]] float scale0 = 0.f;
+  if constexpr (KV == 2) {
+    scale0 = scale_of(t0); scale1 = scale_of(t1); scale2 = scale_of(t2);
+    issue_codes(0, t0); issue_codes(1, t1); issue_codes(2, t2);
+  } else if constexpr (Q8) {
     // through registers: the three chunks are requested together, converted and written, and
     // the first barrier finds all of them in the ring
     const ChunkRegs c0 = load_chunk(t0), c1 = load_chunk(t1), c2 = load_chunk(t2);
-    if constexpr (KV != 0) join_scales();
     commit_chunk(0, c0); commit_chunk(1, c1); commit_chunk(2, c2);
   } else {
     issue_chunk(0, row_at(t0)); issue_chunk(1, row_at(t1)); issue_chunk(2, row_at(t2));
@@ -538,7 +558,7 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
     asm volatile("" : "+v"(ones));   // kept in four registers (the compiler would rebuild it in every step)
   }
   // everything older than chunks 1 and 2 is in: Q, the descriptors and tokens, chunk 0 (Q8: all three chunks)
-  if constexpr (CODES) wait_vmcnt<0>(); else wait_vmcnt<2 * kDmaPerChunk>();
+  if constexpr (Q8) wait_vmcnt<0>(); else if constexpr (KV == 2) wait_vmcnt<2>(); else wait_vmcnt<2 * kDmaPerChunk>();
   [[maybe_unused]] float c_lane = c;           // KV: softmax scale of this lane's query, its and K's powers of two taken out
   [[maybe_unused]] int q_power = 0;
   if constexpr (KV != 0) {
@@ -548,8 +568,9 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
 #pragma unroll
       for (int e = 0; e < 4; ++e) mx = fmaxf(mx, fmaxf(fabsf(__uint_as_float(q_raw[t][e] << 16)), fabsf(__uint_as_float(q_raw[t][e] & 0xffff0000u))));
     q_power = power_to_14(fmaxf(mx, other_half(mx)));
-    if constexpr (!CODES) join_scales();
+    join_scales();
     if (wide_range) ps.far = queries;
+    if constexpr (KV == 2) convert_chunk(0, scale0);
     c_lane = ldexpf(c, -(q_power + k_power));
   }
 #pragma unroll
@@ -790,11 +811,16 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
       d0 = load_desc(min(end, last));
       if constexpr (!FIRST) {
         [[maybe_unused]] unsigned r0 = 0, r1 = 0;
-        if constexpr (CODES) { cr0 = load_chunk(tokn0); cr1 = load_chunk(tokn1); }
-        else { r0 = row_at(tokn0); r1 = row_at(tokn1); asm volatile("" : "+v"(r0), "+v"(r1)); }   // (formed before the registers are loaded again)
+        if constexpr (Q8) { cr0 = load_chunk(tokn0); cr1 = load_chunk(tokn1); }
+        else if constexpr (KV == 2) {
+          r0 = (unsigned)tokn0; r1 = (unsigned)tokn1;
+          scale1 = scale_of(tokn0); scale2 = scale_of(tokn1);
+          asm volatile("" : "+v"(r0), "+v"(r1));
+        } else { r0 = row_at(tokn0); r1 = row_at(tokn1); asm volatile("" : "+v"(r0), "+v"(r1)); }   // (formed before the registers are loaded again)
         tokn0 = load_tok(2 * ph + 3); tokn1 = load_tok(2 * ph + 4);
         // the chunks of phase ph + 1, into the slots of chunks 2 ph - 4 and 2 ph - 3
-        if constexpr (!CODES) { issue_chunk(2 * ph + 1, r0); issue_chunk(2 * ph + 2, r1); }
+        if constexpr (KV == 2) { issue_codes(2 * ph + 1, (int)r0); issue_codes(2 * ph + 2, (int)r1); }
+        else if constexpr (!Q8) { issue_chunk(2 * ph + 1, r0); issue_chunk(2 * ph + 2, r1); }
       }
     }
 #pragma unroll
@@ -809,7 +835,11 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
     // for its own), so after the barrier the slots of chunks 2 ph - 3 and 2 ph - 2 are free.
     wait_vmcnt<0>();
     if (!next) return false;
-    if constexpr (CODES && !FIRST) {
+    if constexpr (KV == 2) {
+      convert_chunk(2 * ph + 1, scale1); convert_chunk(2 * ph + 2, scale2);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    if constexpr (Q8 && !FIRST) {
       // (their slots held chunks 2 ph - 4 and 2 ph - 3, which nobody has read since the
       // barrier that ended phase ph - 1; the writes are complete before this phase's barrier)
       commit_chunk(2 * ph + 1, cr0); commit_chunk(2 * ph + 2, cr1);

@@ -221,8 +221,10 @@ litevar_status launch_blocks(Blocks& w, const char* what, Launch launch) {
 enum Route { kGather, kInKernel, kCopy };
 Route route_of(const litevar_plan* plan) {
   if (plan->waves_per_group != 16 || plan->patches_per_wave == 1 || (int64_t)plan->kv_len * 128 >= ((int64_t)1 << 31)) return kGather;
+  int64_t seen = 0;
+  for (int k = 0; k < plan->q_scale_end; ++k) seen += (int64_t)plan->scales[k] * plan->scales[k];
   const int64_t streamed = plan->n_union_keys / (plan->n_head_groups > 0 ? plan->n_head_groups : 1);
-  return 4 * streamed <= 5 * (2 * (int64_t)plan->kv_len) ? kInKernel : kCopy;
+  return 4 * streamed <= 5 * seen ? kInKernel : kCopy;
 }
 
 // (the stride of an axis with one entry is never used, and is what it is)
