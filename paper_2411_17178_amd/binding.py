@@ -5,6 +5,7 @@ binding passes their data pointers and the current stream handle to the library.
 """
 import contextlib
 import ctypes as C
+import math
 import os
 from array import array
 from itertools import chain
@@ -499,20 +500,18 @@ _CROSS_ATTN_KV8_FWD = C.CFUNCTYPE(C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
                                   C.c_void_p, C.c_float, C.c_void_p, C.c_size_t, C.c_void_p)
 
 
-def _on_device(device, stream):
-    """Context in which calls and allocations go to `device` and to `stream` (None: that device's current stream): its
-    address, and a context manager or None where both already are the current ones."""
+# (torch's own way to the current stream's address, without a Stream object: 2.3 us less per call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _elsewhere(device, stream):
+    """The context in which a call for tensors on `device` and for `stream` runs, allocations included; None: the current
+    device and its current stream already are what is wanted."""
     if stream is not None:
-        return stream.cuda_stream, torch.cuda.stream(stream)
-    address = torch.cuda.current_stream(device).cuda_stream
-    return address, None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-
-
-def _call(context, fn):
-    if context is None:
-        return fn()
-    with context:
-        return fn()
+        assert stream.device == device, "the stream belongs to another device than the tensors"
+        return torch.cuda.stream(stream)
+    return None if device.index == _current_device() else torch.cuda.device(device)
 
 
 def _check_lens(lens, B, device):
@@ -524,10 +523,14 @@ def _check_lens(lens, B, device):
 
 
 def _workspace(workspace, need, device):
+    """(address, bytes) of the caller's workspace, whose size the library checks, or of one of need() bytes."""
     if workspace is None:
-        return torch.empty(need, dtype=torch.uint8, device=device)
+        n = need()
+        if n == 0:
+            return None, None, 0
+        workspace = torch.empty(n, dtype=torch.uint8, device=device)
     assert workspace.device == device and workspace.is_contiguous()
-    return workspace
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def litevar_kv8_blocks(segments):
@@ -559,6 +562,11 @@ class KV8Cache:
         for s in self.segments:
             self.offsets.append(self.offsets[-1] + s)
 
+        # sides of the scales, where all segments are squares (what a plan's scales are compared with)
+        self.sides = [math.isqrt(s) for s in self.segments]
+        if any(r * r != s for r, s in zip(self.sides, self.segments)):
+            self.sides = None
+
     def _pointers(self):
         return self.k8.data_ptr(), self.k_scale.data_ptr(), self.v8.data_ptr(), self.v_scale.data_ptr()
 
@@ -574,21 +582,24 @@ def litevar_kv8_cache(segments, B, H, device="cuda"):
 def litevar_kv8_store(cache, k, v, segments=None, lens=None, stream=None):
     """Quantise k, v [B, H, n, 64] (bf16 or fp32) into the cache's segments [begin, end) (default: all of them).
     lens: optional int32 CUDA tensor [B], the tokens of each row's sequence that count, from the cache's first."""
+    device = cache.device
+    context = _elsewhere(device, stream)
+    if context is not None:
+        with context:
+            return litevar_kv8_store(cache, k, v, segments, lens)
     begin, end = (0, len(cache.segments)) if segments is None else segments
     assert 0 <= begin < end <= len(cache.segments)
     dt = _DTYPES.get(k.dtype)
     if dt is None or v.dtype != k.dtype:
         raise TypeError(f"unsupported dtypes {k.dtype}, {v.dtype}")
-    assert k.device == v.device == cache.device
+    assert k.device == device and v.device == device
     B, H = cache.B, cache.H
-    assert k.shape == v.shape == (B, H, cache.offsets[end] - cache.offsets[begin], 64)
+    shape = k.shape
+    assert shape == (B, H, cache.offsets[end] - cache.offsets[begin], 64) and v.shape == shape
     assert k.stride() == v.stride(), "k and v must share strides"
-    lens_ptr = _check_lens(lens, B, cache.device)
-    address, context = _on_device(cache.device, stream)
     k8, k_scale, v8, v_scale = cache._pointers()
-    fn = load_library().kv8_store
-    rc = _call(context, lambda: fn(cache._segments, len(cache.segments), begin, end, k.data_ptr(), v.data_ptr(), dt, _strides(k),
-                                   B, H, 64, lens_ptr, k8, k_scale, v8, v_scale, address))
+    rc = load_library().kv8_store(cache._segments, len(cache.segments), begin, end, k.data_ptr(), v.data_ptr(), dt, _strides(k), B, H, 64,
+                                  _check_lens(lens, B, device), k8, k_scale, v8, v_scale, _raw_stream(device.index))
     if rc != 0:
         _check(rc)
     return cache
@@ -597,18 +608,20 @@ def litevar_kv8_store(cache, k, v, segments=None, lens=None, stream=None):
 def litevar_kv8_load(cache, segments=None, out=None, stream=None):
     """(k, v): the rows of the cache's segments [begin, end) (default: all) as bf16 [B, H, L, 64]; other rows are not
     written.  out: optional pair of such tensors."""
+    context = _elsewhere(cache.device, stream)
+    if context is not None:
+        with context:
+            return litevar_kv8_load(cache, segments, out)
     begin, end = (0, len(cache.segments)) if segments is None else segments
-    address, context = _on_device(cache.device, stream)
     if out is None:
-        out = _call(context, lambda: tuple(torch.empty(cache.k8.shape, dtype=torch.bfloat16, device=cache.device) for _ in range(2)))
-        context = _on_device(cache.device, stream)[1]
+        out = tuple(torch.empty(cache.k8.shape, dtype=torch.bfloat16, device=cache.device) for _ in range(2))
     for t in out:
         assert t.device == cache.device and t.dtype == torch.bfloat16 and t.shape == cache.k8.shape and t.is_contiguous()
     k8, k_scale, v8, v_scale = (C.c_void_p(p) for p in cache._pointers())
-    _check(_call(context, lambda: load_library().litevar_kv8_load(
+    _check(load_library().litevar_kv8_load(
         cache._segments, C.c_int32(len(cache.segments)), C.c_int32(begin), C.c_int32(end), k8, k_scale, v8, v_scale,
         C.c_int32(cache.B), C.c_int32(cache.H), C.c_int32(64), C.c_void_p(out[0].data_ptr()), C.c_void_p(out[1].data_ptr()),
-        C.c_void_p(address))))
+        _stream_handle(None)))
     return out
 
 
@@ -622,34 +635,34 @@ def litevar_windowed_attn_kv8_fwd(plan, q, cache, sm_scale, out=None, cfg_share=
     """Windowed attention of q [B, H, q_len, 64] (bf16) on an 8-bit cache whose segments are the plan's scales (those
     that the plan's queries see have been stored).  workspace: an uint8 CUDA tensor of
     litevar_windowed_attn_kv8_workspace_bytes() bytes (allocated per call when omitted)."""
+    device = q.device
+    assert device == cache.device
+    context = _elsewhere(device, stream)
+    if context is not None:
+        with context:
+            return litevar_windowed_attn_kv8_fwd(plan, q, cache, sm_scale, out, cfg_share, workspace)
     handle = plan.handle
     if q.dtype != torch.bfloat16:
         raise TypeError(f"unsupported dtype {q.dtype}")
-    assert q.device == cache.device
     B, H, Lq, D = shape = q.shape
     assert Lq == handle.q_len and (B, H, D) == (cache.B, cache.H, 64)
-    assert len(cache.segments) == handle.n_scales and all(s == handle.scales[i] ** 2 for i, s in enumerate(cache.segments)), \
-        "the cache's segments must be the plan's scales"
+    assert cache.sides == handle.scales[:handle.n_scales], "the cache's segments must be the plan's scales"
     flags, share_ptr = 0, None
     if cfg_share is not None:
-        assert cfg_share.device == q.device and cfg_share.dtype == torch.uint8 and cfg_share.is_contiguous()
+        assert cfg_share.device == device and cfg_share.dtype == torch.uint8 and cfg_share.is_contiguous()
         assert cfg_share.shape == (H, handle.n_scales)
         flags, share_ptr = FLAG_CFG_SHARE, cfg_share.data_ptr()
-    address, context = _on_device(q.device, stream)
+    if out is None:
+        out = torch.empty_like(q)
+    assert out.shape == shape and out.dtype == q.dtype and out.device == device
+    keep, work_ptr, work_bytes = _workspace(workspace, lambda: litevar_windowed_attn_kv8_workspace_bytes(plan, B, H), device)
     k8, k_scale, v8, v_scale = cache._pointers()
-    fn = load_library().attn_kv8_fwd
-
-    def call():
-        o = torch.empty_like(q) if out is None else out
-        assert o.shape == shape and o.dtype == q.dtype and o.device == q.device
-        need = litevar_windowed_attn_kv8_workspace_bytes(plan, B, H)
-        w = _workspace(workspace, need, q.device) if need else None
-        rc = fn(C.addressof(handle), q.data_ptr(), k8, k_scale, v8, v_scale, o.data_ptr(), B, H, D, _strides(q), _strides(o),
-                sm_scale, share_ptr, flags, w.data_ptr() if need else None, w.numel() * w.element_size() if need else 0, address)
-        if rc != 0:
-            _check(rc)
-        return o
-    return _call(context, call)
+    rc = load_library().attn_kv8_fwd(C.addressof(handle), q.data_ptr(), k8, k_scale, v8, v_scale, out.data_ptr(), B, H, D, _strides(q),
+                                     _strides(out), sm_scale, share_ptr, flags, work_ptr, work_bytes,
+                                     _raw_stream(device.index))
+    if rc != 0:
+        _check(rc)
+    return out
 
 
 def litevar_cross_attn_workspace_bytes(B, H, H_kv, q_len, kv_len):
@@ -659,54 +672,61 @@ def litevar_cross_attn_workspace_bytes(B, H, H_kv, q_len, kv_len):
     return n.value
 
 
-def _cross_attn(q, H_kv, kv_len, lens, out, workspace, stream, call):
-    B, H, q_len, D = shape = q.shape
-    lens_ptr = _check_lens(lens, B, q.device)
-    address, context = _on_device(q.device, stream)
-
-    def run():
-        o = torch.empty_like(q) if out is None else out
-        assert o.shape == shape and o.dtype == q.dtype and o.device == q.device
-        need = litevar_cross_attn_workspace_bytes(B, H, H_kv, q_len, kv_len)
-        w = _workspace(workspace, need, q.device) if need else None
-        rc = call(o, lens_ptr, w.data_ptr() if need else None, w.numel() * w.element_size() if need else 0, address)
-        if rc != 0:
-            _check(rc)
-        return o
-    return _call(context, run)
-
-
 def litevar_cross_attn_fwd(q, k, v, sm_scale, lens=None, out=None, workspace=None, stream=None):
     """out[B, H, q_len, 64] = attention of q to the first lens[b] (default: all) of the kv_len rows of k, v
     [B, H_kv, kv_len, 64], H a multiple of H_kv; zeros where lens[b] is 0.  bf16 or fp32.  lens: int32 CUDA tensor [B].
     workspace: an uint8 CUDA tensor of litevar_cross_attn_workspace_bytes() bytes (allocated per call when omitted)."""
-    dt = _DTYPES.get(q.dtype)
-    if dt is None or k.dtype != q.dtype or v.dtype != q.dtype:
-        raise TypeError(f"unsupported dtypes {q.dtype}, {k.dtype}, {v.dtype}")
-    assert q.is_cuda and k.device == v.device == q.device
-    B, H, q_len, D = q.shape
-    assert k.dim() == 4 and k.shape[0] == B and k.shape[3] == D and v.shape == k.shape
+    device, dtype = q.device, q.dtype
+    dt = _DTYPES.get(dtype)
+    if dt is None or k.dtype != dtype or v.dtype != dtype:
+        raise TypeError(f"unsupported dtypes {dtype}, {k.dtype}, {v.dtype}")
+    assert q.is_cuda and k.device == device and v.device == device
+    context = _elsewhere(device, stream)
+    if context is not None:
+        with context:
+            return litevar_cross_attn_fwd(q, k, v, sm_scale, lens, out, workspace)
+    B, H, q_len, D = shape = q.shape
+    kv_shape = k.shape
+    assert len(kv_shape) == 4 and kv_shape[0] == B and kv_shape[3] == D and v.shape == kv_shape
     assert k.stride() == v.stride(), "k and v must share strides"
-    H_kv, kv_len = k.shape[1], k.shape[2]
-    fn = load_library().cross_attn_fwd
-    return _cross_attn(q, H_kv, kv_len, lens, out, workspace, stream, lambda o, lens_ptr, w, w_bytes, address: fn(
-        q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), B, H, H_kv, q_len, kv_len, D, dt, _strides(q), _strides(k),
-        _strides(o), lens_ptr, sm_scale, w, w_bytes, address))
+    H_kv, kv_len = kv_shape[1], kv_shape[2]
+    if out is None:
+        out = torch.empty_like(q)
+    assert out.shape == shape and out.dtype == dtype and out.device == device
+    keep, work_ptr, work_bytes = _workspace(workspace, lambda: litevar_cross_attn_workspace_bytes(B, H, H_kv, q_len, kv_len), device)
+    rc = load_library().cross_attn_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), B, H, H_kv, q_len, kv_len, D, dt,
+                                       _strides(q), _strides(k), _strides(out), _check_lens(lens, B, device), sm_scale, work_ptr,
+                                       work_bytes, _raw_stream(device.index))
+    if rc != 0:
+        _check(rc)
+    return out
 
 
 def litevar_cross_attn_kv8_fwd(q, cache, sm_scale, lens=None, out=None, workspace=None, stream=None):
     """litevar_cross_attn_fwd on an 8-bit cache of one segment; q bf16."""
+    device = q.device
     if q.dtype != torch.bfloat16:
         raise TypeError(f"unsupported dtype {q.dtype}")
-    assert q.device == cache.device
-    B, H, q_len, D = q.shape
+    assert device == cache.device
+    context = _elsewhere(device, stream)
+    if context is not None:
+        with context:
+            return litevar_cross_attn_kv8_fwd(q, cache, sm_scale, lens, out, workspace)
+    B, H, q_len, D = shape = q.shape
     assert B == cache.B and D == 64
     assert len(cache.segments) == 1, "cross attention reads a cache of one segment"
-    fn = load_library().cross_attn_kv8_fwd
+    H_kv, kv_len = cache.H, cache.kv_len
+    if out is None:
+        out = torch.empty_like(q)
+    assert out.shape == shape and out.dtype == q.dtype and out.device == device
+    keep, work_ptr, work_bytes = _workspace(workspace, lambda: litevar_cross_attn_workspace_bytes(B, H, H_kv, q_len, kv_len), device)
     k8, k_scale, v8, v_scale = cache._pointers()
-    return _cross_attn(q, cache.H, cache.kv_len, lens, out, workspace, stream, lambda o, lens_ptr, w, w_bytes, address: fn(
-        q.data_ptr(), k8, k_scale, v8, v_scale, o.data_ptr(), B, H, cache.H, q_len, cache.kv_len, D, _strides(q), _strides(o),
-        lens_ptr, sm_scale, w, w_bytes, address))
+    rc = load_library().cross_attn_kv8_fwd(q.data_ptr(), k8, k_scale, v8, v_scale, out.data_ptr(), B, H, H_kv, q_len, kv_len, D,
+                                           _strides(q), _strides(out), _check_lens(lens, B, device), sm_scale, work_ptr, work_bytes,
+                                           _raw_stream(device.index))
+    if rc != 0:
+        _check(rc)
+    return out
 
 
 def litevar_peak_copy(src, dst, stream=None):

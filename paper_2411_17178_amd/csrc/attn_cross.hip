@@ -18,6 +18,7 @@ constexpr int kRows = 32;                      // rows per workgroup: the column
 constexpr int kWaves = 4;
 constexpr int kBlock = LITEVAR_KV8_BLOCK;      // keys per turn
 constexpr int kPitch = 68;                     // floats per row of the joining buffer
+constexpr int kMaxParts = 1024;                // of the key axis
 
 // An exponent that is added to a reference beyond this loses bits that show (codes: the V scales; see k_cross_tiles).
 constexpr float kFarCodes = 0x1p12f;
@@ -34,7 +35,7 @@ struct CrossArgs {
   int parts;                                   // of the key axis
   int scale_blocks;                            // of a (batch, kv head)
   uint32_t q_magic, tiles_magic, hkv_magic, parts_magic, pairs_magic;   // see divmod_by
-  uint32_t first_block;
+  uint32_t first_block, rows_magic;
   int groups, by_xcd; uint32_t groups_magic;   // k_cross_tiles: workgroups of a pair, how they are laid out
   float* part_o; float2* part_ml;              // [item][32][64] and [item][32] (largest score, sum), item = workgroup
 };
@@ -127,8 +128,8 @@ __global__ __launch_bounds__(kWaves * 64) void k_cross_rows(CrossArgs a, float c
 
   float m = -INFINITY, L = 0.f;                // the row's reference; this lane's share of the sum
   f32x16 O[2] = {f32x16{}, f32x16{}};
-  // scores of 32 keys -> probabilities, with the reference moved to their largest
-  auto softmax = [&](f32x16& S, int key0) {
+  // scores of 32 keys -> probabilities, with the reference moved to their largest; returns what that multiplies sums by
+  auto softmax = [&](f32x16& S, int key0) -> float {
     const int left = n_keys - key0 - 4 * hh;
     float mx = -INFINITY;
 #pragma unroll
@@ -138,14 +139,16 @@ __global__ __launch_bounds__(kWaves * 64) void k_cross_rows(CrossArgs a, float c
     }
     mx = fmaxf(mx, other_half(mx));
     const float to = fmaxf(m, mx);
+    float alpha = 1.f;
     if (__builtin_amdgcn_ballot_w64(to > m) != 0) {
-      const float alpha = m > -INFINITY ? __builtin_amdgcn_exp2f((m - to) * c) : 1.f;
+      alpha = m > -INFINITY ? __builtin_amdgcn_exp2f((m - to) * c) : 1.f;
       m = to; L *= alpha;
 #pragma unroll
       for (int e = 0; e < 16; ++e) { O[0][e] *= alpha; O[1][e] *= alpha; }
     }
 #pragma unroll
     for (int e = 0; e < 16; ++e) S[e] = __builtin_amdgcn_exp2f((S[e] - m) * c);
+    return alpha;
   };
 
   if constexpr (KIND == kF32) {
@@ -180,53 +183,93 @@ __global__ __launch_bounds__(kWaves * 64) void k_cross_rows(CrossArgs a, float c
       }
     }
   } else {
+    constexpr bool CODES = KIND == kCodes;
+    constexpr int kTurn = CODES ? 64 : 32;     // keys of a turn: 4 KiB of K and as much of V per wave
+    constexpr int kPerBlock = kBlock / kTurn;
     const __bf16* q = (const __bf16*)a.q + q_at;
     bf16x8 qf[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) qf[t] = as_bf16x8(*(const uint4*)(q + 8 * t));
-    unsigned char* const Vs = smem + wave * 32 * 128;    // this wave's 32 V rows in bf16
-    const int64_t scale_at = KIND == kCodes ? (int64_t)bj * a.scale_blocks : 0;
-    for (int blk = begin + wave; blk < end; blk += kWaves) {
-      float ks = 1.f, vs = 1.f;
-      if constexpr (KIND == kCodes) { ks = a.k_scale[scale_at + blk]; vs = a.v_scale[scale_at + blk]; }
-#pragma unroll 1
-      for (int key0 = kBlock * blk; key0 < min(n_keys, kBlock * (blk + 1)); key0 += 32) {
-        const int64_t k_row = (int64_t)min(key0 + n, n_keys - 1) * a.ks[2];
+    unsigned char* const Vs = smem + wave * kTurn * kRow;          // this wave's V rows of a turn in bf16
+    const int64_t scale_at = CODES ? (int64_t)bj * a.scale_blocks : 0;
+    // A turn's K rows as the first product takes them, its V rows in coalesced pieces (a row behind the last key counts as the
+    // last one, with probability 0), its scales.  The next turn's are requested before this one's are used.
+    struct Turn { u32x4 k[4], v[4]; float ks, vs; };
+    const int last = n_keys - 1, turns = min(end * kPerBlock, (n_keys + kTurn - 1) / kTurn);
+    auto load = [&](int turn) -> Turn {
+      Turn x;
+      const int key0 = turn * kTurn;
+      x.ks = x.vs = 1.f;
+      if constexpr (CODES) {
+        x.ks = a.k_scale[scale_at + turn]; x.vs = a.v_scale[scale_at + turn];
+        const int8_t *K = (const int8_t*)a.k + kv_at + (int64_t)key0 * 64, *V = (const int8_t*)a.v + kv_at + (int64_t)key0 * 64;
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) x.k[2 * half + i] = *(const u32x4*)(K + min(32 * half + n, last - key0) * 64 + 32 * hh + 16 * i);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.v[i] = *(const u32x4*)(V + min(16 * i + (lane >> 2), last - key0) * 64 + 16 * (lane & 3));
+      } else {
+        const __bf16* K = (const __bf16*)a.k + kv_at + (int64_t)min(key0 + n, last) * a.ks[2] + 32 * hh;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) x.k[t] = *(const u32x4*)(K + 8 * t);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          x.v[i] = *(const u32x4*)((const __bf16*)a.v + kv_at + (int64_t)min(key0 + 8 * i + (lane >> 3), last) * a.ks[2] + 8 * (lane & 7));
+      }
+      return x;
+    };
+    int turn = begin * kPerBlock + wave;
+    Turn next;
+    if (turn < turns) next = load(turn);
+    for (; turn < turns; turn += kWaves) {
+      const Turn x = next;
+      if (turn + kWaves < turns) next = load(turn + kWaves);
+      if constexpr (CODES) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const unsigned row = 16u * i + ((unsigned)lane >> 2), p = 2u * ((unsigned)lane & 3u), sw = dense_swizzle(row);
+          const unsigned w0 = x.v[i][0], w1 = x.v[i][1], w2 = x.v[i][2], w3 = x.v[i][3];
+          *(bf16x8*)(Vs + row * kRow + ((p ^ sw) << 4)) = codes_to_bf16(w0, w1);
+          *(bf16x8*)(Vs + row * kRow + (((p + 1u) ^ sw) << 4)) = codes_to_bf16(w2, w3);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const unsigned row = 8u * i + ((unsigned)lane >> 3);
+          *(u32x4*)(Vs + row * kRow + ((((unsigned)lane & 7u) ^ dense_swizzle(row)) << 4)) = x.v[i];
+        }
+      }
+      asm volatile("" ::: "memory");           // (the rows of V are read by other lanes than wrote them; LDS keeps a wave's order)
+      f32x16 P[2];                             // codes: the turn's products with V, which the V scale multiplies
+      if constexpr (CODES) { P[0] = f32x16{}; P[1] = f32x16{}; }
+#pragma unroll
+      for (int half = 0; half < kTurn / 32; ++half) {
+        const int key0 = turn * kTurn + 32 * half;
+        if (half > 0 && key0 > last) break;
         f32x16 S = f32x16{};
-        if constexpr (KIND == kCodes) {
-          const u32x4* kp = (const u32x4*)((const int8_t*)a.k + kv_at + k_row + 32 * hh);
-          const u32x4 x0 = kp[0], x1 = kp[1];
-          S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(codes_to_bf16(x0[0], x0[1]), qf[0], S, 0, 0, 0);
-          S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(codes_to_bf16(x0[2], x0[3]), qf[1], S, 0, 0, 0);
-          S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(codes_to_bf16(x1[0], x1[1]), qf[2], S, 0, 0, 0);
-          S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(codes_to_bf16(x1[2], x1[3]), qf[3], S, 0, 0, 0);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) S[e] *= ks;
-          // V codes: four lanes per row, sixteen rows per load
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int row = 16 * i + (lane >> 2), key = key0 + row, p = 2 * (lane & 3);
-            const u32x4 x = *(const u32x4*)((const int8_t*)a.v + kv_at + (int64_t)min(key, n_keys - 1) * a.ks[2] + 8 * p);
-            const bf16x8 lo = codes_to_bf16(x[0], x[1]), hi = codes_to_bf16(x[2], x[3]);
-            *(bf16x8*)(Vs + row * 128 + (((unsigned)p ^ dense_swizzle((unsigned)row)) << 4)) = lo;
-            *(bf16x8*)(Vs + row * 128 + (((unsigned)(p + 1) ^ dense_swizzle((unsigned)row)) << 4)) = hi;
+        for (int t = 0; t < 4; ++t) {
+          bf16x8 kf;
+          if constexpr (CODES) {
+            const unsigned lo = x.k[2 * half + (t >> 1)][2 * (t & 1)], hi = x.k[2 * half + (t >> 1)][2 * (t & 1) + 1];
+            kf = codes_to_bf16(lo, hi);
+          } else {
+            kf = __builtin_bit_cast(bf16x8, x.k[t]);
           }
-        } else {
-          const __bf16* kp = (const __bf16*)a.k + kv_at + k_row + 32 * hh;
+          S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[t], S, 0, 0, 0);
+        }
+        if constexpr (CODES) {
 #pragma unroll
-          for (int t = 0; t < 4; ++t)
-            S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(kp + 8 * t)), qf[t], S, 0, 0, 0);
-          // V: eight lanes per row, eight rows per load; a row behind the last key counts as the last one, with
-          // probability 0
+          for (int e = 0; e < 16; ++e) S[e] *= x.ks;
+        }
+        const float alpha = softmax(S, key0);
+        if constexpr (CODES) {
+          if (half > 0 && __builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int row = 8 * i + (lane >> 3);
-            const uint4 x = *(const uint4*)((const __bf16*)a.v + kv_at + (int64_t)min(key0 + row, n_keys - 1) * a.ks[2] + 8 * (lane & 7));
-            *(uint4*)(Vs + row * 128 + ((((unsigned)lane & 7u) ^ dense_swizzle((unsigned)row)) << 4)) = x;
+            for (int e = 0; e < 16; ++e) { P[0][e] *= alpha; P[1][e] *= alpha; }
           }
         }
-        softmax(S, key0);
-        asm volatile("" ::: "memory");         // (the rows of V are read by other lanes than wrote them; LDS keeps a wave's order)
         bf16x8 pb[2];
         float sum = L;
 #pragma unroll
@@ -237,8 +280,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_cross_rows(CrossArgs a, float c
           for (int e = 0; e < 8; e += 2) sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pb[t][e], pb[t][e + 1]}, kOnes, sum, false);
         }
         L = sum;
-        f32x16 P[2];
-        if constexpr (KIND == kCodes) { P[0] = f32x16{}; P[1] = f32x16{}; } else { P[0] = O[0]; P[1] = O[1]; }
+        f32x16 (&acc)[2] = CODES ? P : O;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -246,21 +288,19 @@ __global__ __launch_bounds__(kWaves * 64) void k_cross_rows(CrossArgs a, float c
             s16x8 v8;
 #pragma unroll
             for (int jj = 0; jj < 2; ++jj) {
-              const unsigned l16 = (unsigned)lane & 15u, row = 16u * t + 8u * jj + 4u * (unsigned)hh + (l16 >> 2);
+              const unsigned l16 = (unsigned)lane & 15u, row = 32u * half + 16u * t + 8u * jj + 4u * (unsigned)hh + (l16 >> 2);
               const unsigned piece = 4u * dt + 2u * (((unsigned)lane >> 4) & 1u) + ((l16 & 3u) >> 1);
-              const s16x4 x = lds_read_tr16(Vs + row * 128 + ((piece ^ dense_swizzle(row)) << 4) + 8u * (l16 & 1u));
+              const s16x4 y = lds_read_tr16(Vs + row * kRow + ((piece ^ dense_swizzle(row)) << 4) + 8u * (l16 & 1u));
 #pragma unroll
-              for (int e = 0; e < 4; ++e) v8[4 * jj + e] = x[e];
+              for (int e = 0; e < 4; ++e) v8[4 * jj + e] = y[e];
             }
-            P[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v8), pb[t], P[dt], 0, 0, 0);
+            acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v8), pb[t], acc[dt], 0, 0, 0);
           }
-        asm volatile("" ::: "memory");
-        if constexpr (KIND == kCodes) {
+      }
+      asm volatile("" ::: "memory");
+      if constexpr (CODES) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) { O[0][e] = fmaf(P[0][e], vs, O[0][e]); O[1][e] = fmaf(P[1][e], vs, O[1][e]); }
-        } else {
-          O[0] = P[0]; O[1] = P[1];
-        }
+        for (int e = 0; e < 16; ++e) { O[0][e] = fmaf(P[0][e], x.vs, O[0][e]); O[1][e] = fmaf(P[1][e], x.vs, O[1][e]); }
       }
     }
   }
@@ -281,6 +321,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_cross_rows(CrossArgs a, float c
   float x[8];
   const float2 ml = join(kWaves, c, [&](int s) { return ML[s * kRows + row]; },
                          [&](int s) { return (const float*)smem + (s * kRows + row) * kPitch + 8 * dims; }, x);
+  if (row0 + row >= a.rows) return;
   if (a.parts > 1) {
     if (dims == 0) a.part_ml[(int64_t)item * kRows + row] = ml;
     float* p = a.part_o + ((int64_t)item * kRows + row) * 64 + 8 * dims;
@@ -288,7 +329,6 @@ __global__ __launch_bounds__(kWaves * 64) void k_cross_rows(CrossArgs a, float c
     *(float4*)(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
     return;
   }
-  if (row0 + row >= a.rows) return;
   const float inv = ml.y > 0.f ? 1.f / ml.y : 0.f;       // (no key: zeros)
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] *= inv;
@@ -643,31 +683,70 @@ void k_cross_tiles(CrossArgs a, float c) {
   for (; __builtin_expect(bad != 0, 0); bad &= bad - 1) row_again<KIND>(a, c, b, j, bj, n_keys, row0 + __builtin_ctzll(bad));
 }
 
-// Joins the parts of one tile of rows: a workgroup per (batch, kv head, tile).
+// Joins the parts of a row: a workgroup per row, thread t dims 4 (t % 16) .. + 3 of the parts t / 16, + 16, ...
 template <int KIND>
 __global__ __launch_bounds__(256) void k_cross_join(CrossArgs a, float c) {
-  const int row = threadIdx.x & 31, dims = threadIdx.x >> 5;
-  int tile, bj, b, j;
-  const uint32_t at = a.first_block + blockIdx.x;
-  divmod_by(at, (uint32_t)a.tiles, a.tiles_magic, bj, tile);
+  __shared__ float weight[kMaxParts], wave_m[4], wave_l[4];
+  __shared__ __align__(16) float4 sums[16][16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int bj, r, b, j;
+  divmod_by(a.first_block + blockIdx.x, (uint32_t)a.rows, a.rows_magic, bj, r);
   divmod_by((uint32_t)bj, (uint32_t)a.Hkv, a.hkv_magic, b, j);
-  if (tile * kRows + row >= a.rows) return;
-  const int64_t first = (int64_t)at * a.parts;
-  float x[8];
-  const float2 ml = join(a.parts, c, [&](int s) { return a.part_ml[(first + s) * kRows + row]; },
-                         [&](int s) { return a.part_o + ((first + s) * kRows + row) * 64 + 8 * dims; }, x);
-  const float inv = ml.y > 0.f ? 1.f / ml.y : 0.f;
+  const int tile = r / kRows, row = r % kRows;
+  const int64_t first = ((int64_t)bj * a.tiles + tile) * a.parts;
+  float m = -INFINITY, own_m[kMaxParts / 256], own_l[kMaxParts / 256];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] *= inv;
-  store_row<KIND>(a, b, j, tile * kRows + row, dims, x);
+  for (int i = 0; i < kMaxParts / 256; ++i) {
+    const int s = tid + 256 * i;
+    const float2 ml = s < a.parts ? a.part_ml[(first + s) * kRows + row] : make_float2(-INFINITY, 0.f);
+    own_m[i] = ml.x; own_l[i] = ml.y;
+    m = fmaxf(m, ml.x);
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+  if (lane == 0) wave_m[wave] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(wave_m[0], wave_m[1]), fmaxf(wave_m[2], wave_m[3]));
+  float l = 0.f;
+#pragma unroll
+  for (int i = 0; i < kMaxParts / 256; ++i) {
+    // (a part without keys: its products were not written, and do not count)
+    const float f = own_m[i] > -INFINITY ? __builtin_amdgcn_exp2f((own_m[i] - m) * c) : 0.f;
+    l = fmaf(own_l[i], f, l);
+    weight[tid + 256 * i] = own_m[i] > -INFINITY ? f : -1.f;
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) l += __shfl_xor(l, d);
+  if (lane == 0) wave_l[wave] = l;
+  __syncthreads();
+  l = (wave_l[0] + wave_l[1]) + (wave_l[2] + wave_l[3]);
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int s = tid >> 4; s < a.parts; s += 16) {
+    const float f = weight[s];
+    const float4 y = *(const float4*)(a.part_o + ((first + s) * kRows + row) * 64 + 4 * (tid & 15));
+    if (f >= 0.f) { x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w); }
+  }
+  sums[tid >> 4][tid & 15] = x;
+  __syncthreads();
+  if (tid >= 8) return;
+  float out[8] = {};
+  for (int s = 0; s < 16; ++s)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) out[e] += ((const float*)&sums[s][2 * tid])[e];
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) out[e] *= inv;
+  store_row<KIND>(a, b, j, r, tid, out);
 }
 
 namespace {
 
-// Parts of the key axis: as many as give about four workgroups per CU, none of fewer than four blocks.
+// Parts of the key axis: as many as give about two workgroups per CU, none of fewer than four blocks, one per wave.  (16 kv
+// heads, 30 011 keys in 8 bits, workgroups in all: 256 24.0 us, 384 22.5, 512 20.3, 1024 22.6, 2048 29.6.)
 int parts_of(int64_t tiles, int64_t kv_len) {
   const int64_t blocks = (kv_len + kBlock - 1) / kBlock;
-  int64_t p = tiles > 0 ? 1024 / tiles : 1;
+  int64_t p = tiles > 0 ? 512 / tiles : 1;
   if (p > blocks / kWaves) p = blocks / kWaves;
   return (int)(p < 1 ? 1 : p);
 }
@@ -722,7 +801,7 @@ template <int KIND> litevar_status launch(CrossArgs& a, float c, hipStream_t st)
         hipLaunchKernelGGL(k_cross_rows<KIND>, dim3(n), dim3(kWaves * 64), 0, st, a, c);
       })) return s;
   if (a.parts == 1) return LITEVAR_OK;
-  return launch_in_parts(tiles, 256, "cross attention join launch", [&](int64_t first, unsigned n) {
+  return launch_in_parts((int64_t)a.B * a.Hkv * a.rows, 256, "cross attention join launch", [&](int64_t first, unsigned n) {
     a.first_block = (uint32_t)first;
     hipLaunchKernelGGL(k_cross_join<KIND>, dim3(n), dim3(256), 0, st, a, c);
   });
@@ -758,7 +837,7 @@ litevar_status cross_attention(CrossArgs& a, Kind kind, int32_t B, int32_t H, in
   a.parts = parts_of(tiles, kv_len);
   a.scale_blocks = (kv_len + kBlock - 1) / kBlock;
   a.q_magic = magic_of(q_len); a.tiles_magic = magic_of(a.tiles); a.hkv_magic = magic_of(H_kv); a.parts_magic = magic_of(a.parts);
-  a.pairs_magic = magic_of((int64_t)B * H_kv);
+  a.pairs_magic = magic_of((int64_t)B * H_kv); a.rows_magic = magic_of(a.rows);
   a.part_o = (float*)d_workspace;
   a.part_ml = (float2*)((char*)d_workspace + (size_t)tiles * a.parts * kRows * 64 * 4);
   const float c = sm_scale * 1.4426950408889634f;
