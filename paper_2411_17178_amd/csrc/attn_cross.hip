@@ -107,7 +107,8 @@ __device__ inline float2 join(int n, float c, Ml ml, O o, float (&x)[8]) {
 // (bf16, codes) or straight from memory (fp32, a value per lane).  Softmax with the running largest score as the reference,
 // subtracted before the scale is applied, so that scores of any size keep their differences.
 template <int KIND>
-__global__ __launch_bounds__(kWaves * 64) void k_cross_rows(CrossArgs a, float c) {
+__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(KIND == kBf16 ? 4 : 3, KIND == kBf16 ? 4 : 3)))
+void k_cross_rows(CrossArgs a, float c) {
   __shared__ __align__(16) unsigned char smem[kWaves * kRows * kPitch * 4 + kWaves * kRows * 8];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int n = lane & 31, hh = lane >> 5;
@@ -161,25 +162,39 @@ __global__ __launch_bounds__(kWaves * 64) void k_cross_rows(CrossArgs a, float c
     }
     const float* K = (const float*)a.k + kv_at + 32 * hh;
     const float* V = (const float*)a.v + kv_at + n;
-    for (int key0 = kBlock * begin + 32 * wave; key0 < min(n_keys, kBlock * end); key0 += 32 * kWaves) {
-      const float* kp = K + (int64_t)min(key0 + n, n_keys - 1) * a.ks[2];
-      float kf[32];
+    const int last = n_keys - 1, stop = min(n_keys, kBlock * end);
+    // V of a step is requested ahead of its score products, K of the next step behind them: each has half a step (2048
+    // cycles of the matrix pipe) to arrive.
+    float kf[32];
+    auto load_k = [&](int key0) {
+      const float* kp = K + (int64_t)min(key0 + n, last) * a.ks[2];
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
         const float4 x = *(const float4*)(kp + 4 * t);
         kf[4 * t] = x.x; kf[4 * t + 1] = x.y; kf[4 * t + 2] = x.z; kf[4 * t + 3] = x.w;
       }
+    };
+    int key0 = kBlock * begin + 32 * wave;
+    if (key0 < stop) load_k(key0);
+    for (; key0 < stop; key0 += 32 * kWaves) {
+      float vf[2][16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {           // (probability 0 where the key is clamped)
+        const float* vp = V + (int64_t)min(key0 + 8 * (e >> 2) + 4 * hh + (e & 3), last) * a.ks[2];
+        vf[0][e] = vp[0]; vf[1][e] = vp[32];
+      }
       f32x16 S = f32x16{};
 #pragma unroll
       for (int t = 0; t < 32; ++t) S = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[t], qf[t], S, 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      load_k(key0 + 32 * kWaves < stop ? key0 + 32 * kWaves : key0);
+      __builtin_amdgcn_sched_barrier(0);
       softmax(S, key0);
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int key = key0 + 8 * (e >> 2) + 4 * hh + (e & 3);
-        const float* vp = V + (int64_t)min(key, n_keys - 1) * a.ks[2];   // (probability 0 where the key is clamped)
         L += S[e];
-        O[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(vp[0], S[e], O[0], 0, 0, 0);
-        O[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(vp[32], S[e], O[1], 0, 0, 0);
+        O[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[0][e], S[e], O[0], 0, 0, 0);
+        O[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[1][e], S[e], O[1], 0, 0, 0);
       }
     }
   } else {
@@ -342,7 +357,8 @@ __device__ inline void row_again(const CrossArgs& a, float c, int b, int j, int 
   wait_vmcnt<0>();
   const int lane = lane_of_wave();
   const Row qr = row_at(a, j, row);
-  const __bf16* q = (const __bf16*)a.q + b * a.qs[0] + qr.h * a.qs[1] + qr.i * a.qs[2];
+  using T = std::conditional_t<KIND == kF32, float, __bf16>;
+  const T* q = (const T*)a.q + b * a.qs[0] + qr.h * a.qs[1] + qr.i * a.qs[2];
   const int64_t kv_at = b * a.ks[0] + j * a.ks[1];
   float m = -INFINITY, l = 0.f, o = 0.f;
   for (int key0 = 0; key0 < n_keys; key0 += 64) {
@@ -351,16 +367,23 @@ __device__ inline void row_again(const CrossArgs& a, float c, int b, int j, int 
     float s = 0.f;
 #pragma unroll 1
     for (int d = 0; d < 64; d += 8) {
-      bf16x8 x;
-      if constexpr (KIND == kCodes) {
-        const uint2 w = *(const uint2*)((const int8_t*)a.k + at + d);
-        x = codes_to_bf16(w.x, w.y);
-      } else {
-        x = as_bf16x8(*(const uint4*)((const __bf16*)a.k + at + d));
-      }
-      const bf16x8 y = as_bf16x8(*(const uint4*)(q + d));
+      float x[8];
+      if constexpr (KIND == kF32) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s = fmaf((float)x[e], (float)y[e], s);
+        for (int e = 0; e < 8; ++e) x[e] = ((const float*)a.k)[at + d + e];
+      } else {
+        bf16x8 w;
+        if constexpr (KIND == kCodes) {
+          const uint2 u = *(const uint2*)((const int8_t*)a.k + at + d);
+          w = codes_to_bf16(u.x, u.y);
+        } else {
+          w = as_bf16x8(*(const uint4*)((const __bf16*)a.k + at + d));
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (float)w[e];
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = fmaf(x[e], (float)q[d + e], s);
     }
     float vs = 1.f;
     if constexpr (KIND == kCodes) { s *= a.k_scale[scale_at]; vs = a.v_scale[scale_at]; }
@@ -377,11 +400,11 @@ __device__ inline void row_again(const CrossArgs& a, float c, int b, int j, int 
     l = fmaf(l, alpha, sum); o *= alpha; m = to;
     for (int i = 0; i < min(64, n_keys - key0); ++i) {
       const int64_t v_at = kv_at + (int64_t)(key0 + i) * a.ks[2] + lane;
-      const float v = KIND == kCodes ? (float)((const int8_t*)a.v)[v_at] * vs : (float)((const __bf16*)a.v)[v_at];
+      const float v = KIND == kCodes ? (float)((const int8_t*)a.v)[v_at] * vs : (float)((const T*)a.v)[v_at];
       o = fmaf(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(p), i)), v, o);
     }
   }
-  ((__bf16*)a.o + b * a.os[0] + qr.h * a.os[1] + qr.i * a.os[2])[lane] = (__bf16)(o * (1.f / l));
+  ((T*)a.o + b * a.os[0] + qr.h * a.os[1] + qr.i * a.os[2])[lane] = (T)(o * (1.f / l));
 }
 
 // Many rows: NWV waves of one (batch, kv head), each with 32 rows, share the K and V rows, which pass through LDS in chunks
@@ -683,6 +706,180 @@ void k_cross_tiles(CrossArgs a, float c) {
   for (; __builtin_expect(bad != 0, 0); bad &= bad - 1) row_again<KIND>(a, c, b, j, bj, n_keys, row0 + __builtin_ctzll(bad));
 }
 
+// a lane's half of a K row of 256 bytes, eight pieces; issued only, a wait must precede the first use
+template <int AT> __device__ inline void read_k_rows(unsigned k, u32x4 (&r)[8]) {
+#pragma unroll
+  for (int t = 0; t < 8; t += 4)
+    asm volatile("ds_read_b128 %0, %4 offset:%8\n\tds_read_b128 %1, %5 offset:%8\n\t"
+                 "ds_read_b128 %2, %6 offset:%8\n\tds_read_b128 %3, %7 offset:%8"
+                 : "=&v"(r[t]), "=&v"(r[t + 1]), "=&v"(r[t + 2]), "=&v"(r[t + 3])
+                 : "v"(k ^ (16u * t)), "v"(k ^ (16u * t + 16u)), "v"(k ^ (16u * t + 32u)), "v"(k ^ (16u * t + 48u)), "i"(AT) : "memory");
+}
+
+// Many rows in fp32: as k_cross_tiles, 32 keys to a chunk.  The matrix pipe bounds it: 64 instructions of 64 cycles for 32
+// keys x 32 rows, beside which vector instructions of other waves do not run (two waves per SIMD take twice as long as one), so
+// that each of these counts: no maximum, no mask but in the last chunk, one multiply-add and one addition per score.  K pieces are
+// swizzled by row (sixteen rows put a piece into sixteen places); V rows are read whole, lane n dimensions 2 n and 2 n + 1.
+// Four buffers: 64 KiB leave two workgroups to a CU, so that a launch of a few per CU is dealt out as they end (three to a CU, all
+// resident at once: 2240 rows, 32 pairs of 301 and 153 keys 58.9 us, so 56.4).
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void k_cross_tiles_f32(CrossArgs a, float c) {
+  constexpr int NWV = 4, kKeys = 32, kRowF = 256, kBuf = 2 * kKeys * kRowF, kBufs = 4, kTransfers = kKeys / (4 * NWV);
+  __shared__ __align__(1024) unsigned char smem[kBufs * kBuf];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int n = lane & 31, hh = lane >> 5;
+  int tile, bj, b, j;
+  const uint32_t block = a.first_block + blockIdx.x;
+  if (a.by_xcd) {
+    divmod_by(block >> 3, (uint32_t)a.groups, a.groups_magic, bj, tile);
+    bj = 8 * bj + (int)(block & 7);
+    if (bj >= a.B * a.Hkv) return;
+  } else {
+    divmod_by(block, (uint32_t)(a.B * a.Hkv), a.pairs_magic, tile, bj);
+  }
+  divmod_by((uint32_t)bj, (uint32_t)a.Hkv, a.hkv_magic, b, j);
+  const int n_keys = keys_of(a, b), row0 = (tile * NWV + wave) * kRows;
+  const bool working = row0 < a.rows;          // (uniform)
+  float qf[32];
+  {
+    const Row qr = row_at(a, j, min(row0 + n, a.rows - 1));
+    const float* qp = (const float*)a.q + b * a.qs[0] + qr.h * a.qs[1] + qr.i * a.qs[2] + 32 * hh;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      const float4 x = *(const float4*)(qp + 4 * t);
+      qf[4 * t] = x.x; qf[4 * t + 1] = x.y; qf[4 * t + 2] = x.z; qf[4 * t + 3] = x.w;
+    }
+  }
+  __builtin_amdgcn_sched_barrier(0);           // (the loads of Q stay ahead of the transfers, which are counted below)
+  const int n_chunks = (n_keys + kKeys - 1) / kKeys;
+  // a transfer: four rows, sixteen lanes each
+  const int64_t kv_at = b * a.ks[0] + j * a.ks[1];
+  const unsigned row_bytes = (unsigned)a.ks[2] * 4u;
+  auto issue_chunk = [&](int chunk, int buf) {
+    const int64_t base = (kv_at + (int64_t)chunk * kKeys * a.ks[2]) * 4;
+#pragma unroll
+    for (int i = 0; i < kTransfers; ++i) {
+      const int r0 = 4 * (kTransfers * wave + i), r = r0 + (lane >> 4);
+      const unsigned from = (unsigned)min(r, n_keys - 1 - kKeys * chunk) * row_bytes, piece = (unsigned)lane & 15u;
+      unsigned char* dst = smem + buf * kBuf + r0 * kRowF;
+      __builtin_amdgcn_global_load_lds((global_void*)((const unsigned char*)a.k + base + (from + ((piece ^ ((unsigned)r & 15u)) << 4))), (lds_void*)dst, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((global_void*)((const unsigned char*)a.v + base + (from + (piece << 4))), (lds_void*)(dst + kKeys * kRowF), 16, 0, 0);
+    }
+  };
+  const unsigned k_at = lds_addr(smem) + (unsigned)n * kRowF + (((8u * (unsigned)hh) ^ ((unsigned)n & 15u)) << 4);
+  const unsigned v_at = lds_addr(smem) + kKeys * kRowF + 4u * (unsigned)hh * kRowF + 8u * (unsigned)n;
+
+  f32x16 O[2] = {f32x16{}, f32x16{}};          // row m of tile dt: dimension 2 m + dt
+  float negm = 0.f, L = 0.f;                   // minus the reference (base 2), this lane's part of the row sum
+  uint64_t far = 0;                            // lanes whose reference has been beyond kFarReference
+  if (n_chunks > 0) {
+    issue_chunk(0, 0);
+    if (n_chunks > 1) issue_chunk(1, 1);
+    if (n_chunks > 2) { issue_chunk(2, 2); wait_vmcnt<4 * kTransfers>(); } else wait_vmcnt<0>();
+    asm volatile("s_barrier" ::: "memory");
+  }
+  auto one = [&](int chunk, auto which) -> bool {
+    constexpr int p = decltype(which)::value, AT = p * kBuf;
+    const bool more = chunk + 1 < n_chunks;
+    if (working) {
+      u32x4 kr[8];
+      u32x2 vr[16];
+      read_k_rows<AT>(k_at, kr);
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        asm volatile("ds_read_b64 %0, %4 offset:%5\n\tds_read_b64 %1, %4 offset:%6\n\t"
+                     "ds_read_b64 %2, %4 offset:%7\n\tds_read_b64 %3, %4 offset:%8"
+                     : "=&v"(vr[e]), "=&v"(vr[e + 1]), "=&v"(vr[e + 2]), "=&v"(vr[e + 3])
+                     : "v"(v_at), "i"(AT + 2 * e * kRowF), "i"(AT + (2 * e + 1) * kRowF), "i"(AT + (2 * e + 2) * kRowF),
+                       "i"(AT + (2 * e + 3) * kRowF) : "memory");
+      asm volatile("s_waitcnt lgkmcnt(0)"
+                   : "+v"(kr[0]), "+v"(kr[1]), "+v"(kr[2]), "+v"(kr[3]), "+v"(kr[4]), "+v"(kr[5]), "+v"(kr[6]), "+v"(kr[7]) : : "memory");
+      asm volatile("" : "+v"(vr[0]), "+v"(vr[1]), "+v"(vr[2]), "+v"(vr[3]), "+v"(vr[4]), "+v"(vr[5]), "+v"(vr[6]), "+v"(vr[7]),
+                        "+v"(vr[8]), "+v"(vr[9]), "+v"(vr[10]), "+v"(vr[11]), "+v"(vr[12]), "+v"(vr[13]), "+v"(vr[14]), "+v"(vr[15]));
+      f32x16 S = f32x16{};
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const u32x4 w = kr[t];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const unsigned u = w[e];
+          S = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(u), qf[4 * t + e], S, 0, 0, 0);
+        }
+      }
+      if (!more) {                             // (uniform; kept a branch)
+        int left = n_keys - chunk * kKeys - 4 * hh;
+        asm volatile("" : "+v"(left));
+#pragma unroll
+        for (int e = 0; e < 16; ++e) S[e] = 8 * (e >> 2) + (e & 3) < left ? S[e] : -INFINITY;
+      }
+      auto largest = [&]() {                   // of the row, over both of its lanes
+        float mx = S[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) mx = fmaxf(mx, S[e]);
+        return fmaxf(mx, other_half(mx));
+      };
+      if (chunk == 0) {
+        negm = -largest() * c;
+        far = is_far(negm);
+      }
+      float P[16], sum;
+      auto exponentials = [&]() {
+        sum = L;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) { P[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[e], c, negm)); sum += P[e]; }
+      };
+      exponentials();
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(sum > kMostSum) != 0, 0)) {
+        const float now = sum + other_half(sum), before = L + other_half(L);
+        float to = __builtin_fmaf(largest(), c, negm);
+        if (before > 0.f) to = fmaxf(to, __builtin_amdgcn_logf(before));       // (base 2)
+        const float shift = now > kMostSum ? rintf(to) : 0.f, alpha = __builtin_amdgcn_exp2f(-shift);
+        negm -= shift; L *= alpha;
+        far |= is_far(negm);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) { O[0][e] *= alpha; O[1][e] *= alpha; }
+        exponentials();
+      }
+      L = sum;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const unsigned u0 = vr[e][0], u1 = vr[e][1];
+        O[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(u0), P[e], O[0], 0, 0, 0);
+        O[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(u1), P[e], O[1], 0, 0, 0);
+      }
+    }
+    if (!more) return false;
+    if (chunk + 2 < n_chunks) wait_vmcnt<2 * kTransfers>(); else wait_vmcnt<0>();      // (the next chunk is in)
+    asm volatile("s_barrier" ::: "memory");
+    if (chunk + 3 < n_chunks) issue_chunk(chunk + 3, (p + 3) % kBufs);
+    return true;
+  };
+  for (int chunk = 0; n_chunks > 0; chunk += kBufs) {
+    if (!one(chunk, std::integral_constant<int, 0>{})) break;
+    if (!one(chunk + 1, std::integral_constant<int, 1>{})) break;
+    if (!one(chunk + 2, std::integral_constant<int, 2>{})) break;
+    if (!one(chunk + 3, std::integral_constant<int, 3>{})) break;
+  }
+  if (!working) return;
+  const float l = L + other_half(L), inv = l > 0.f ? 1.f / l : 0.f;            // (no key: zeros)
+  const int row = row0 + (lane_of_wave() & 31);
+  float any = 0.f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) { O[0][e] *= inv; O[1][e] *= inv; any += O[0][e] + O[1][e]; }
+  if (row < a.rows) {
+    const Row qr = row_at(a, j, row);
+    // O[dt][e]: dimension 2 (8 (e / 4) + 4 hh + e % 4) + dt
+    float* op = (float*)a.o + b * a.os[0] + qr.h * a.os[1] + qr.i * a.os[2] + 8 * (lane_of_wave() >> 5);
+#pragma unroll
+    for (int e = 0; e < 16; e += 2)
+      *(float4*)(op + 16 * (e >> 2) + 2 * (e & 3)) = make_float4(O[0][e], O[1][e], O[0][e + 1], O[1][e + 1]);
+  }
+  // (rows formed again as in k_cross_tiles)
+  uint64_t bad = (far | __builtin_amdgcn_ballot_w64(not_finite(any))) & __builtin_amdgcn_ballot_w64(row < a.rows);
+  bad = (bad | (bad >> 32)) & 0xffffffffull;
+  for (; __builtin_expect(bad != 0, 0); bad &= bad - 1) row_again<kF32>(a, c, b, j, bj, n_keys, row0 + __builtin_ctzll(bad));
+}
+
 // Joins the parts of a row: a workgroup per row, thread t dims 4 (t % 16) .. + 3 of the parts t / 16, + 16, ...
 template <int KIND>
 __global__ __launch_bounds__(256) void k_cross_join(CrossArgs a, float c) {
@@ -780,21 +977,22 @@ litevar_status strides_of(const int64_t* s, int B, int heads, int64_t n, int D, 
 
 template <int KIND> litevar_status launch(CrossArgs& a, float c, hipStream_t st) {
   const int64_t tiles = (int64_t)a.B * a.Hkv * a.tiles;
-  if constexpr (KIND != kF32) {
-    // (64 rows of K or V span less than 4 GiB, see issue_chunk)
-    if (a.parts == 1 && a.tiles > 1 && a.ks[2] < (1 << 24)) {
-      const int nwv = a.tiles > 4 ? 8 : 4;
-      const int64_t pairs = (int64_t)a.B * a.Hkv;
-      a.groups = (a.tiles + nwv - 1) / nwv; a.groups_magic = magic_of(a.groups);
-      a.by_xcd = 9 * pairs >= 8 * ((pairs + 7) / 8 * 8);       // (288 pairs of 2240 rows: 93.0 us pair by pair in turn, 91.7 so)
-      const int64_t blocks = (a.by_xcd ? (pairs + 7) / 8 * 8 : pairs) * a.groups;
-      if (blocks > 0x7fffffff) return fail(LITEVAR_E_UNSUPPORTED, "grid too large");
-      return launch_in_parts(blocks, nwv * 64, "cross attention launch", [&](int64_t first, unsigned n) {
-        a.first_block = (uint32_t)first;
-        if (nwv == 8) hipLaunchKernelGGL((k_cross_tiles<8, KIND>), dim3(n), dim3(512), 0, st, a, c);
-        else hipLaunchKernelGGL((k_cross_tiles<4, KIND>), dim3(n), dim3(256), 0, st, a, c);
-      });
-    }
+  // (64 rows of K or V span less than 4 GiB, see issue_chunk)
+  if (a.parts == 1 && a.tiles > 1 && a.ks[2] < (1 << 23)) {
+    const int nwv = KIND != kF32 && a.tiles > 4 ? 8 : 4;
+    const int64_t pairs = (int64_t)a.B * a.Hkv;
+    a.groups = (a.tiles + nwv - 1) / nwv; a.groups_magic = magic_of(a.groups);
+    a.by_xcd = 9 * pairs >= 8 * ((pairs + 7) / 8 * 8);         // (288 pairs of 2240 rows: 93.0 us pair by pair in turn, 91.7 so)
+    const int64_t blocks = (a.by_xcd ? (pairs + 7) / 8 * 8 : pairs) * a.groups;
+    if (blocks > 0x7fffffff) return fail(LITEVAR_E_UNSUPPORTED, "grid too large");
+    return launch_in_parts(blocks, nwv * 64, "cross attention launch", [&](int64_t first, unsigned n) {
+      a.first_block = (uint32_t)first;
+      if constexpr (KIND == kF32) {
+        hipLaunchKernelGGL(k_cross_tiles_f32, dim3(n), dim3(256), 0, st, a, c);
+      }
+      else if (nwv == 8) hipLaunchKernelGGL((k_cross_tiles<8, KIND>), dim3(n), dim3(512), 0, st, a, c);
+      else hipLaunchKernelGGL((k_cross_tiles<4, KIND>), dim3(n), dim3(256), 0, st, a, c);
+    });
   }
   if (litevar_status s = launch_in_parts(tiles * a.parts, kWaves * 64, "cross attention launch", [&](int64_t first, unsigned n) {
         a.first_block = (uint32_t)first;
