@@ -6,6 +6,7 @@
 // One workgroup = four waves = 32 rows of one (batch, kv head) and one part of the key axis; the waves take the part's
 // blocks of 64 keys (32 in fp32) in turn and join their results through LDS.  With several parts, each leaves its sums
 // in the workspace and a second launch joins them.
+#include <cmath>
 #include <cstring>
 #include <type_traits>
 
@@ -18,7 +19,7 @@ constexpr int kRows = 32;                      // rows per workgroup: the column
 constexpr int kWaves = 4;
 constexpr int kBlock = LITEVAR_KV8_BLOCK;      // keys per turn
 constexpr int kPitch = 68;                     // floats per row of the joining buffer
-constexpr int kMaxParts = 1024;                // of the key axis
+constexpr int kMaxParts = 512;                 // of the key axis
 
 // An exponent that is added to a reference beyond this loses bits that show (codes: the V scales; see k_cross_tiles).
 constexpr float kFarCodes = 0x1p12f;
@@ -939,13 +940,32 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossArgs a, float c) {
 
 namespace {
 
-// Parts of the key axis: as many as give about two workgroups per CU, none of fewer than four blocks, one per wave.  (16 kv
-// heads, 30 011 keys in 8 bits, workgroups in all: 256 24.0 us, 384 22.5, 512 20.3, 1024 22.6, 2048 29.6.)
-int parts_of(int64_t tiles, int64_t kv_len) {
+// Parts of the key axis for `tiles` tiles of 32 rows, `rows` rows in all.  A workgroup without parts needs 4.2 us and 0.36
+// per block of 64 keys (bf16); parts divide that, and cost a second launch of 3.3 us and 0.27 ns per row and part for the sums that
+// they leave.  That is least at sqrt(1355 blocks / rows) parts; with fewer than three, few blocks, or a tile for nearly every
+// CU there is nothing to gain.  (Tiles, rows, blocks), bf16, us without / with as many parts as given here: (1, 1, 64) 26.2 / 8.7 (64);
+// (8, 256, 64) 27.9 / 10.4 (18); (32, 1024, 64) 31.4 / 13.4 (9); (128, 4096, 64) 36.5 / 25.6 (4); (128, 4096, 256) 124 / 56 (4);
+// declined: (64, 64, 4) 5.8 / 7.9 (4); (256, 256, 64) 40.2 / 46.2 (4); (256, 6400, 64) 39.7 / 41.4 (4).
+int parts_of(int64_t tiles, int64_t rows, int64_t kv_len) {
   const int64_t blocks = (kv_len + kBlock - 1) / kBlock;
-  int64_t p = tiles > 0 ? 512 / tiles : 1;
-  if (p > blocks / kWaves) p = blocks / kWaves;
-  return (int)(p < 1 ? 1 : p);
+  if (tiles < 1 || tiles >= 200 || blocks <= 8) return 1;
+  int64_t most = blocks / 16 < 64 ? 64 : blocks / 16;
+  if (most > kMaxParts) most = kMaxParts;
+  if (most > blocks) most = blocks;
+  if (most > 512 / tiles) most = 512 / tiles;
+  int64_t p = (int64_t)std::sqrt(1355.0 * (double)blocks / (double)rows);
+  if (p > most) p = most;
+  return p < 3 ? 1 : (int)p;
+}
+
+// Whether rows share K and V through LDS (k_cross_tiles, k_cross_tiles_f32): from so many tiles of 32 rows on, and two or
+// more of a pair.  (Tiles, keys), us, shared / each tile its own: bf16 (352, 1024) 17.9 / 16.6, (512, 1024) 18.2 / 24.0, (1024, 1024)
+// 20.1 / 42.3; codes (512, 1024) 22.2 / 20.4, (960, 1024) 28.7 / 32.0, (2048, 1024) 31.8 / 53.9; fp32 (960, 1024) 131 / 97, (1408, 1024) 136 /
+// 133, (2048, 1024) 139 / 181.
+template <int KIND> bool shares_rows(const CrossArgs& a) {
+  // (64 rows of K or V span less than 4 GiB, see issue_chunk)
+  const int64_t least = KIND == kF32 ? 1800 : KIND == kCodes ? 768 : 448;
+  return a.parts == 1 && a.tiles > 1 && a.ks[2] < (1 << 23) && (int64_t)a.B * a.Hkv * a.tiles >= least;
 }
 
 uint32_t magic_of(int64_t n) { return (uint32_t)(((uint64_t)1 << 32) / (uint64_t)(n > 1 ? n : 1) - (n <= 1)); }
@@ -977,9 +997,11 @@ litevar_status strides_of(const int64_t* s, int B, int heads, int64_t n, int D, 
 
 template <int KIND> litevar_status launch(CrossArgs& a, float c, hipStream_t st) {
   const int64_t tiles = (int64_t)a.B * a.Hkv * a.tiles;
-  // (64 rows of K or V span less than 4 GiB, see issue_chunk)
-  if (a.parts == 1 && a.tiles > 1 && a.ks[2] < (1 << 23)) {
-    const int nwv = KIND != kF32 && a.tiles > 4 ? 8 : 4;
+  if (shares_rows<KIND>(a)) {
+    // Eight waves to a workgroup read K and V half as often; four waste less on few tiles and leave less of the chip idle:
+    // (tiles of a pair, pairs), 1024 keys, eight / four: (8, 64) 21.4 / 18.2; (22, 64) 23.0 / 25.2; (8, 256) 25.9 / 27.8; (22, 480) 106 / 118.
+    // On codes eight spill registers: (8, 480) 53.0 / 54.1, (8, 256) 33.8 / 31.8.
+    const int nwv = KIND == kBf16 && a.tiles > 4 && (int64_t)a.B * a.Hkv * ((a.tiles + 7) / 8) >= 192 ? 8 : 4;
     const int64_t pairs = (int64_t)a.B * a.Hkv;
     a.groups = (a.tiles + nwv - 1) / nwv; a.groups_magic = magic_of(a.groups);
     a.by_xcd = 9 * pairs >= 8 * ((pairs + 7) / 8 * 8);         // (288 pairs of 2240 rows: 93.0 us pair by pair in turn, 91.7 so)
@@ -990,7 +1012,7 @@ template <int KIND> litevar_status launch(CrossArgs& a, float c, hipStream_t st)
       if constexpr (KIND == kF32) {
         hipLaunchKernelGGL(k_cross_tiles_f32, dim3(n), dim3(256), 0, st, a, c);
       }
-      else if (nwv == 8) hipLaunchKernelGGL((k_cross_tiles<8, KIND>), dim3(n), dim3(512), 0, st, a, c);
+      else if (nwv == 8) hipLaunchKernelGGL((k_cross_tiles<8, kBf16>), dim3(n), dim3(512), 0, st, a, c);
       else hipLaunchKernelGGL((k_cross_tiles<4, KIND>), dim3(n), dim3(256), 0, st, a, c);
     });
   }
@@ -1032,7 +1054,7 @@ litevar_status cross_attention(CrossArgs& a, Kind kind, int32_t B, int32_t H, in
   a.B = B; a.H = H; a.Hkv = H_kv; a.G = H / H_kv; a.q_len = q_len; a.kv_len = kv_len;
   a.rows = a.G * q_len; a.tiles = (a.rows + kRows - 1) / kRows;
   const int64_t tiles = tiles_of(B, H, H_kv, q_len);
-  a.parts = parts_of(tiles, kv_len);
+  a.parts = parts_of(tiles, (int64_t)B * H * q_len, kv_len);
   a.scale_blocks = (kv_len + kBlock - 1) / kBlock;
   a.q_magic = magic_of(q_len); a.tiles_magic = magic_of(a.tiles); a.hkv_magic = magic_of(H_kv); a.parts_magic = magic_of(a.parts);
   a.pairs_magic = magic_of((int64_t)B * H_kv); a.rows_magic = magic_of(a.rows);
@@ -1056,7 +1078,7 @@ litevar_status litevar_cross_attn_workspace_bytes(int32_t B, int32_t H, int32_t 
                                                   size_t* out_bytes) {
   if (!out_bytes) return fail(LITEVAR_E_INVALID_ARG, "out_bytes is NULL");
   if (litevar_status s = check_shape(B, H, H_kv, q_len, kv_len)) return s;
-  const int64_t tiles = tiles_of(B, H, H_kv, q_len), parts = parts_of(tiles, kv_len);
+  const int64_t tiles = tiles_of(B, H, H_kv, q_len), parts = parts_of(tiles, (int64_t)B * H * q_len, kv_len);
   *out_bytes = parts > 1 ? (size_t)tiles * parts * kRows * (64 * 4 + 8) : 0;
   return LITEVAR_OK;
 }
