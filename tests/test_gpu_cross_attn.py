@@ -77,7 +77,11 @@ SHAPES = [  # B, H, H_kv, q_len, kv_len
     (2, 4, 4, 64, 64), (2, 2, 2, 65, 65), (4, 3, 3, 100, 129), (2, 30, 30, 169, 333), (3, 6, 3, 257, 200),
     (2, 8, 1, 1, 1000), (1, 2, 2, 5, 4099), (2, 8, 2, 3, 9001), (1, 1, 1, 2240, 512), (2, 5, 5, 300, 1),
     (2, 3, 3, 7, 0), (2, 3, 3, 0, 7),
+    # rows that share K and V through LDS, in four and in eight waves; with shared heads
+    (8, 32, 32, 257, 200), (16, 32, 32, 100, 77), (16, 32, 8, 140, 130), (8, 64, 64, 300, 33), (4, 64, 64, 1000, 1), (16, 32, 32, 130, 0),
 ]
+# (rows of a call that share K and V through LDS, whatever the type: 2560 tiles)
+MANY = (16, 32, 130)
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "codes"])
@@ -93,9 +97,10 @@ def test_cross_attention(lv, shape, ragged, kind):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "codes"])
-def test_rows_behind_the_length_are_not_read(lv, kind):
-    B, H, n, L = 6, 3, 40, 150
-    lens = torch.tensor([150, 1, 64, 65, 0, 97], dtype=torch.int32).cuda()
+@pytest.mark.parametrize("B,H,n", [(6, 3, 40), MANY], ids=str)
+def test_rows_behind_the_length_are_not_read(lv, kind, B, H, n):
+    L = 150
+    lens = torch.tensor(([150, 1, 64, 65, 0, 97] + list(range(20, 40)))[:B], dtype=torch.int32).cuda()
     q, k, v = _randn((B, H, n, 64), 5), _randn((B, H, L, 64), 6), _randn((B, H, L, 64), 7)
     for b, m in enumerate(lens.tolist()):
         k[b, :, m:] = float("nan")
@@ -105,7 +110,7 @@ def test_rows_behind_the_length_are_not_read(lv, kind):
     assert bool((out[4] == 0).all())
 
 
-@pytest.mark.parametrize("n", [3, 200])
+@pytest.mark.parametrize("n", [3, 20000])
 def test_lengths_outside_the_axis_are_taken_as_its_ends(lv, n):
     q, k, v = _randn((3, 2, n, 64), 8), _randn((3, 2, 70, 64), 9), _randn((3, 2, 70, 64), 10)
     wild = torch.tensor([1000, -1, 70], dtype=torch.int32).cuda()
@@ -116,10 +121,10 @@ def test_lengths_outside_the_axis_are_taken_as_its_ends(lv, n):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
-@pytest.mark.parametrize("n", [1, 50, 300])
-def test_strides(lv, kind, n):
+@pytest.mark.parametrize("H,n", [(4, 1), (4, 50), (4, 300), (150, 141)])
+def test_strides(lv, kind, H, n):
     """Rows as a fused projection leaves them, K and V of one prompt shared by the batch, an output inside a larger one."""
-    B, H, L = 3, 4, 90
+    B, L = 3, 90
     dtype = torch.float32 if kind == "f32" else torch.bfloat16
     q = _randn((B, n, H, 64), 11, dtype).transpose(1, 2)
     kv = _randn((1, L, 2 * H, 64), 12, dtype)
@@ -133,10 +138,10 @@ def test_strides(lv, kind, n):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "codes"])
-@pytest.mark.parametrize("n", [2, 130])
-def test_peaked_and_far_scores(lv, kind, n):
+@pytest.mark.parametrize("B,H,n", [(2, 2, 2), (2, 2, 130), MANY], ids=str)
+def test_peaked_and_far_scores(lv, kind, B, H, n):
     """Scores of many sizes: one key takes nearly everything, scores fall and rise along the axis."""
-    B, H, L = 2, 2, 300
+    L = 300
     q, k, v = _randn((B, H, n, 64), 13, scale=3.0), _randn((B, H, L, 64), 14, scale=3.0), _randn((B, H, L, 64), 15)
     k = k * torch.linspace(0.01, 2.0, L, device="cuda")[:, None]
     for flip in (False, True):
@@ -146,11 +151,11 @@ def test_peaked_and_far_scores(lv, kind, n):
         plain.assert_close(out, want, tol)
 
 
-@pytest.mark.parametrize("kind", ["bf16", "codes"])
-@pytest.mark.parametrize("n", [1, 100])
-def test_scores_that_fp32_holds_keep_their_differences(lv, kind, n):
-    """Scores around 2^27 whose differences are whole numbers of 2^4: the largest keys win, exactly."""
-    B, H, L = 1, 1, 128
+@pytest.mark.parametrize("kind", ["bf16", "f32", "codes"])
+@pytest.mark.parametrize("B,H,n", [(1, 1, 1), (1, 1, 100), MANY], ids=str)
+def test_scores_that_fp32_holds_keep_their_differences(lv, kind, B, H, n):
+    """Scores around 2^27 whose differences are whole numbers of 2^20: the largest keys win, exactly."""
+    L = 128
     q = torch.zeros(B, H, n, 64, device="cuda")
     q[..., 0] = 2.0 ** 14
     k = torch.zeros(B, H, L, 64, device="cuda")
@@ -158,13 +163,27 @@ def test_scores_that_fp32_holds_keep_their_differences(lv, kind, n):
     k[:, :, ::2, 0] = 126.0 * 64
     v = _randn((B, H, L, 64), 16)
     out, want, tol = _run(lv, kind, q, k, v, None, sm=1.0)
+    if kind == "f32":                                                    # (the scores are exact here: no term of theirs)
+        tol = 2.0 ** -20 * (tol * 0 + v.abs().amax())
+    plain.assert_close(out, want, tol)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("B,H,n", [(1, 2, 40), MANY], ids=str)
+def test_values_near_the_end_of_the_range(lv, kind, B, H, n):
+    """Values of 2^120 and scores that rise along the axis: sums under a reference that moves do not overflow into the
+    result."""
+    L = 200
+    q, k, v = _randn((B, H, n, 64), 30), _randn((B, H, L, 64), 31) * 0.1, _randn((B, H, L, 64), 32) * 2.0 ** 120
+    k = k + q.mean(2, keepdim=True) * torch.linspace(0.0, 30.0, L, device="cuda")[:, None]
+    out, want, tol = _run(lv, kind, q.to(torch.bfloat16).float(), k.to(torch.bfloat16).float(), v.to(torch.bfloat16).float(), None)
     plain.assert_close(out, want, tol)
 
 
 def test_blocks_of_very_different_scales(lv):
     """Blocks of K and V between 2^-110 and 2^110 of one another, blocks of zeros: each counts at its own size."""
-    B, H, L = 1, 6, 64 * 5
-    for n in (1, 40, 290):
+    L = 64 * 5
+    for B, H, n in ((1, 6, 1), (1, 6, 40), (1, 6, 290), (50, 6, 90)):
         q = _randn((B, H, n, 64), 17)
         k, v = _randn((B, H, L, 64), 18), _randn((B, H, L, 64), 19)
         k[:, 0, 64:128] *= 2.0 ** -110
@@ -178,7 +197,7 @@ def test_blocks_of_very_different_scales(lv):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "codes"])
-@pytest.mark.parametrize("shape", [(2, 4, 4, 3, 5000), (2, 4, 4, 200, 300)], ids=str)
+@pytest.mark.parametrize("shape", [(2, 4, 4, 3, 5000), (2, 4, 4, 200, 300), (16, 32, 32, 130, 70)], ids=str)
 def test_workspace_contents_do_not_matter_and_runs_repeat(lv, kind, shape):
     B, H, Hkv, n, L = shape
     need = lv.litevar_cross_attn_workspace_bytes(B, H, Hkv, n, L)
@@ -199,16 +218,16 @@ def test_offsets_beyond_32_bits(lv):
     base = torch.empty(L, heads, 64, dtype=torch.bfloat16, device="cuda")     # 4.6 GB
     base[:, -1] = _randn((L, 64), 24, torch.bfloat16)
     kv = base.view(1, L, heads, 64).transpose(1, 2)[:, -1:]
-    for n in (2, 100):
+    for n in (2, 100, 16000):
         q = _randn((1, 1, n, 64), 25, torch.bfloat16)
         out = lv.litevar_cross_attn_fwd(q, kv, kv, SM)
         want, A, S = plain.attention(q, kv, kv, _keep(None, 1, L), SM)
         plain.assert_close(out, want, _tolerance("bf16", want, A, S, L))
 
 
-@pytest.mark.parametrize("n,L", [(2, 6000), (150, 300)])
-def test_streams_and_graphs(lv, n, L):
-    B, H = 2, 4
+@pytest.mark.parametrize("H,n,L", [(4, 2, 6000), (4, 150, 300), (300, 130, 100)])
+def test_streams_and_graphs(lv, H, n, L):
+    B = 2
     side = torch.cuda.Stream()
     q, k, v = (_randn(s, i, torch.bfloat16) for i, s in enumerate([(B, H, n, 64), (B, H, L, 64), (B, H, L, 64)]))
     cache = lv.litevar_kv8_cache([L], B, H)
