@@ -4,7 +4,11 @@ queries being that scale's tokens and the keys the cache rows of the scales so f
 --asc the unconditional half of the batch reuses the conditional half's attention output
 everywhere (paper Section 3).  Run as
 
-    python -m paper_2411_17178_amd.bench_generation [--workload var_d30_kvstep] [--asc] [--graph]
+    python -m paper_2411_17178_amd.bench_generation [--workload var_d30_kvstep] [--asc] [--graph] [--kv8] [--states N]
+
+--kv8 keeps K and V in an 8-bit cache with block scales: every step stores its scale's rows and attends to the cache.
+--states N adds what a conditioned layer does behind each step, attention to N encoder states (ragged lengths; with --kv8
+from an 8-bit cache of their own, filled once).
 
 Prints one JSON line: microseconds per layer (all steps of one layer), per step, and the
 effective TFLOP/s over the retained (query, key) pairs that were computed.  Inputs are
@@ -24,6 +28,8 @@ def main():
     ap.add_argument("--warmup", type=int, default=3)
     ap.add_argument("--asc", action="store_true", help="share the conditional output everywhere")
     ap.add_argument("--graph", action="store_true", help="replay each layer's steps as one HIP graph")
+    ap.add_argument("--kv8", action="store_true", help="8-bit K/V cache with block scales")
+    ap.add_argument("--states", type=int, default=0, help="encoder states that each step attends to as well")
     ap.add_argument("--batch", type=int, default=0, help="batch size (0 = the workload's)")
     ap.add_argument("--no-hint", action="store_true", help="do not tell the plans the batch size")
     args = ap.parse_args()
@@ -64,8 +70,32 @@ def main():
 
     stream = torch.cuda.Stream()
     with torch.cuda.stream(stream):
-        layer_calls = [gen.prepare(qs, k, v, w.sm_scale, os_, share_all=args.asc, stream=stream)
-                       for qs, k, v, os_ in calls]
+        if args.kv8:
+            work = torch.empty(max(1, gen.kv8_workspace_bytes(B, H)), dtype=torch.uint8, device=dev)
+            rows = [gen.rows(s) for s in range(gen.n_steps)]
+
+            def kv8_steps(qs, k, v, os_):
+                cache = gen.kv8_cache(B, H, dev)
+                return [lambda s=s, lo=lo, hi=hi: gen.step_kv8(s, qs[s], k[:, :, lo:hi], v[:, :, lo:hi], cache, w.sm_scale,
+                                                               out_k=os_[s], share_all=args.asc, workspace=work)
+                        for s, (lo, hi) in enumerate(rows)]
+            layer_calls = [kv8_steps(*c) for c in calls]
+        else:
+            layer_calls = [gen.prepare(qs, k, v, w.sm_scale, os_, share_all=args.asc, stream=stream)
+                           for qs, k, v, os_ in calls]
+        if args.states:
+            lens = torch.randint(args.states // 4, args.states + 1, (B,), generator=g, device=dev, dtype=torch.int32)
+            cross_work = torch.empty(max([1] + [lv.litevar_cross_attn_workspace_bytes(B, H, H, hi - lo, args.states)
+                                                for lo, hi in (gen.rows(s) for s in range(gen.n_steps))]),
+                                     dtype=torch.uint8, device=dev)
+
+            def with_states(steps, qs):
+                k, v = (torch.randn((B, H, args.states, 64), generator=g, device=dev).to(torch.bfloat16) for _ in range(2))
+                states = lv.litevar_kv8_store(lv.litevar_kv8_cache([args.states], B, H, dev), k, v, lens=lens) if args.kv8 else (k, v)
+                outs = [torch.empty_like(x) for x in qs]
+                return [f for step, x, o in zip(steps, qs, outs)
+                        for f in (step, lambda x=x, o=o: gen.cross(x, states, w.sm_scale, lens=lens, out_k=o, workspace=cross_work))]
+            layer_calls = [with_states(steps, c[0]) for steps, c in zip(layer_calls, calls)]
         if args.graph:
             graphs = []
             for lc in layer_calls:
@@ -106,7 +136,7 @@ def main():
         "config": {"workload": w.name + " (all steps)", "scales": list(w.scales), "batch": B,
                    "heads": H, "radius": w.radius, "asc_everywhere": bool(args.asc),
                    "patches_per_group": [int(p.waves_per_group) for p in gen.plans],
-                   "hip_graph": bool(args.graph)}}))
+                   "hip_graph": bool(args.graph), "kv8_cache": bool(args.kv8), "encoder_states": args.states}}))
 
 
 if __name__ == "__main__":

@@ -9,7 +9,9 @@ output in every head and at every scale (paper Section 3: the unconditional work
 at once, the conditional ones store both rows).
 
 Argument marshalling only: the plans are built by litevar_mask_build and every step runs
-litevar_windowed_attn_fwd (litevar_windowed_attn_qkv8_fwd for 8-bit caches).  The calls allocate nothing and never synchronise, so a caller may
+litevar_windowed_attn_fwd (litevar_windowed_attn_qkv8_fwd for 8-bit operands, litevar_kv8_store and
+litevar_windowed_attn_kv8_fwd for an 8-bit cache with block scales, litevar_cross_attn_fwd or
+litevar_cross_attn_kv8_fwd for a conditioned layer's attention to an encoder's states).  The calls allocate nothing and never synchronise, so a caller may
 capture them in a HIP graph (torch.cuda.graph) and replay a whole layer with one launch.
 """
 import torch
@@ -63,6 +65,32 @@ class GenerationLayer:
         return binding.litevar_windowed_attn_qkv8_fwd(self.plans[k], q8_k, q_sz_k, k8_cache, k_sz_cache,
                                                       v8_cache, v_sz_cache, sm_scale, out=out_k,
                                                       cfg_share=share, workspace=workspace, stream=stream)
+
+    def kv8_cache(self, B, H, device="cuda"):
+        """An empty 8-bit cache of this sequence (one scale per block of 64 tokens and head, see litevar_kv8_store)."""
+        return binding.litevar_kv8_cache([s * s for s in self.scales], B, H, device=device)
+
+    def kv8_workspace_bytes(self, B, H):
+        """Bytes of the workspace that step_kv8 needs at most."""
+        return max(binding.litevar_windowed_attn_kv8_workspace_bytes(p, B, H) for p in self.plans)
+
+    def step_kv8(self, k, q_k, k_new, v_new, cache, sm_scale, out_k=None, share_all=False, workspace=None, stream=None):
+        """The step on an 8-bit cache: scale k's rows `k_new`, `v_new` [B, H, s_k^2, 64] (bf16 or fp32) are stored, then its
+        queries `q_k` (bf16) attend to scales 0..k of the cache.  `workspace`: a uint8 CUDA tensor of
+        kv8_workspace_bytes() bytes (allocated per call when omitted)."""
+        binding.litevar_kv8_store(cache, k_new, v_new, (k, k + 1), stream=stream)
+        share = self._share_table(q_k) if share_all else None
+        return binding.litevar_windowed_attn_kv8_fwd(self.plans[k], q_k, cache, sm_scale, out=out_k, cfg_share=share,
+                                                     workspace=workspace, stream=stream)
+
+    @staticmethod
+    def cross(q_k, states, sm_scale, lens=None, out_k=None, workspace=None, stream=None):
+        """A conditioned layer's attention of `q_k` [B, H, n, 64] to an encoder's states, the same at every step:
+        `states` is a pair (k, v) [B, H_kv, len, 64] or an 8-bit cache of one segment."""
+        if isinstance(states, binding.KV8Cache):
+            return binding.litevar_cross_attn_kv8_fwd(q_k, states, sm_scale, lens=lens, out=out_k, workspace=workspace, stream=stream)
+        return binding.litevar_cross_attn_fwd(q_k, states[0], states[1], sm_scale, lens=lens, out=out_k, workspace=workspace,
+                                              stream=stream)
 
     def prepare(self, q_steps, k_cache, v_cache, sm_scale, out_steps, share_all=False, stream=None):
         """Marshal all steps once; returns zero-argument callables, one per step, that
