@@ -386,17 +386,20 @@ __device__ inline float wave_max(float x) {
 }
 
 // The block scales of a (batch, head), dealt to the lanes of a wave: power() brings 127 times the largest finite one
-// below 2^14; wide(): one that is not zero lies more than 2^20 below it.
+// below 2^14; wide: one that is not zero lies more than 2^20 below it.
 struct HeadScales {
-  float largest = 0.f, least = INFINITY;       // of this lane's, and of the whole head behind join()
+  float largest = 0.f, least = INFINITY;       // of this lane's; largest of the whole head behind join()
+  bool wide = false;
   __device__ void add(float x) {
     const bool counts = !not_finite(x);
     largest = counts ? fmaxf(largest, x) : largest;
-    least = counts && x > 0.f ? fminf(least, x) : least;
+    least = x > 0.f ? fminf(least, x) : least;
   }
-  __device__ void join() { largest = wave_max(largest); least = -wave_max(-least); }
+  __device__ void join() {
+    largest = wave_max(largest);
+    wide = __builtin_amdgcn_ballot_w64(least < largest * 0x1p-20f) != 0;
+  }
   __device__ int power() const { return largest > 0x1p120f ? power_to_14(largest) - 7 : power_to_14(127.f * largest); }
-  __device__ bool wide() const { return least < largest * 0x1p-20f; }
 };
 
 }  // namespace lv

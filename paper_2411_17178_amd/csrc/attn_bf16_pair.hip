@@ -303,7 +303,7 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
     head_k.add(first_k); head_v.add(first_v);
     head_k.join(); head_v.join();
     k_power = __builtin_amdgcn_readfirstlane(head_k.power()); v_power = __builtin_amdgcn_readfirstlane(head_v.power());
-    wide_range = head_k.wide() || head_v.wide();
+    wide_range = head_k.wide || head_v.wide;
   };
   // KV = 2: the segment that this wave's next rows begin in (the list goes through the key scales in order); lane k holds
   // scale k's first token and shift
@@ -563,11 +563,17 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
   [[maybe_unused]] float c_lane = c;           // KV: softmax scale of this lane's query, its and K's powers of two taken out
   [[maybe_unused]] int q_power = 0;
   if constexpr (KV != 0) {
-    float mx = 0.f;
+    // (the largest magnitude of the row: bf16 bits without their sign compare as integers, two to a word)
+    typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+    u16x2 top = {0, 0};
 #pragma unroll
     for (int t = 0; t < kQPieces; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) mx = fmaxf(mx, fmaxf(fabsf(__uint_as_float(q_raw[t][e] << 16)), fabsf(__uint_as_float(q_raw[t][e] & 0xffff0000u))));
+      for (int e = 0; e < 4; ++e) {
+        const unsigned w = q_raw[t][e] & 0x7fff7fffu;
+        top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w));
+      }
+    const float mx = __uint_as_float((unsigned)(top.x > top.y ? top.x : top.y) << 16);
     q_power = power_to_14(fmaxf(mx, other_half(mx)));
     join_scales();
     if (wide_range) ps.far = queries;

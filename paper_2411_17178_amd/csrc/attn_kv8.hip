@@ -194,8 +194,12 @@ __global__ __launch_bounds__(W * 64) void k_attn_kv8(AttnArgs a, KV8Scales ks, i
 
 litevar_status launch_attn_kv8(const litevar_plan* pl, const AttnArgs& args, const KV8Scales& scales, hipStream_t st) {
   AttnArgs a = args;
-  // (as the fp32 kernel: patches of one step each would leave three of four waves without work)
-  const int W = pl->n_steps <= (int64_t)pl->n_patches * pl->n_head_groups ? 1 : 4;
+  // Four waves shorten the chain of a patch's steps; one wave per patch where patches have a single step, or where there are so
+  // many that the chip is full of them.  (Patches, steps of one), us, one wave / four: (480, 1) 5.5 / 8.2; (480, 2) 6.1 / 5.8; (1920, 2)
+  // 7.5 / 9.9; (1920, 5) 13.8 / 15.3; (1920, 7.5) 25.4 / 19.8; (4320, 5.9) 37.9 / 39.0; (27 360, 6.8) 147 / 195; two are nowhere better by
+  // more than 8 %.
+  const int64_t patches = (int64_t)pl->n_patches * pl->n_head_groups, all = (int64_t)a.B * a.H * pl->n_patches;
+  const int W = pl->n_steps <= patches || all >= 4000 || (all >= 1500 && pl->n_steps <= 5 * patches) ? 1 : 4;
   const int64_t n_waves = (int64_t)pl->n_groups * pl->waves_per_group;
   const int64_t blocks = spread_over_xcds(a, n_waves, 64);
   if (blocks > 0x7fffffff) return fail(LITEVAR_E_UNSUPPORTED, "grid too large");
