@@ -413,8 +413,12 @@ litevar_status litevar_windowed_attn_qkv8_fwd(const litevar_plan* plan, const in
  *                     that the plan's queries see have to be stored.  d_q, d_o DEVICE bf16 [B, H, q_len, 64] with
  *                     strides as there; d_workspace DEVICE, 256-byte aligned, at least
  *                     litevar_windowed_attn_kv8_workspace_bytes() bytes (NULL where that is 0), contents undefined
- *                     before and after; calls that share a workspace must not overlap.  K and V reach the matrix
- *                     products as bf16(s * code).  Other arguments as litevar_windowed_attn_fwd.
+ *                     before and after; calls that share a workspace must not overlap.  Plans of 16 patches per group
+ *                     form the products in f16: s * code off by 2^-12 relative at most, a weight by 2^-11 relative or
+ *                     2^-21 of the row's sum (as exact as the others where a head's block scales differ by more than
+ *                     2^20, but by a slow path).  Other plans form them from the codes, exactly, and round a weight
+ *                     times its V scale to bf16.  A scale that is not finite reaches the queries that keep one of its
+ *                     block's tokens and no others.  Other arguments as litevar_windowed_attn_fwd.
  * All but litevar_kv8_blocks and the workspace size: asynchronous on `stream`.
  */
 #define LITEVAR_KV8_BLOCK 64
@@ -449,8 +453,9 @@ litevar_status litevar_windowed_attn_kv8_fwd(const litevar_plan* plan, const voi
  *   d_workspace DEVICE, 16-byte aligned, at least litevar_cross_attn_workspace_bytes() bytes (NULL where that is 0),
  *               contents undefined before and after; calls that share a workspace must not overlap
  * litevar_cross_attn_kv8_fwd: the same with K and V in an 8-bit cache of one segment of kv_len tokens (see
- *               litevar_kv8_store; the same lengths), Q and O in bf16.  The codes enter the matrix products exactly, the
- *               scales are applied to fp32 sums.
+ *               litevar_kv8_store; the same lengths), Q and O in bf16.  The codes enter the matrix products exactly, K's
+ *               scales multiply fp32 scores, V's fp32 sums or, relative to the largest (at least 2^-96 of it), the
+ *               probabilities ahead of their rounding to bf16.
  * Inputs must be finite.  Results do not depend on the run (no atomics).  Asynchronous on `stream`.
  */
 litevar_status litevar_cross_attn_workspace_bytes(int32_t B, int32_t H, int32_t H_kv, int32_t q_len, int32_t kv_len,

@@ -514,10 +514,15 @@ def _elsewhere(device, stream):
     return None if device.index == _current_device() else torch.cuda.device(device)
 
 
+def _layout(t):
+    """Element strides of the (B, head, token) axes, None where the tensor is packed."""
+    return None if t.is_contiguous() else _strides(t)
+
+
 def _check_lens(lens, B, device):
     if lens is None:
         return None
-    assert lens.dtype == torch.int32 and lens.shape == (B,) and lens.is_contiguous() and lens.device == device, \
+    assert lens.dtype is torch.int32 and lens.shape == (B,) and lens.is_contiguous() and lens.device == device, \
         "lens: contiguous int32 [B] on the operands' device"
     return lens.data_ptr()
 
@@ -598,7 +603,7 @@ def litevar_kv8_store(cache, k, v, segments=None, lens=None, stream=None):
     assert shape == (B, H, cache.offsets[end] - cache.offsets[begin], 64) and v.shape == shape
     assert k.stride() == v.stride(), "k and v must share strides"
     k8, k_scale, v8, v_scale = cache._pointers()
-    rc = load_library().kv8_store(cache._segments, len(cache.segments), begin, end, k.data_ptr(), v.data_ptr(), dt, _strides(k), B, H, 64,
+    rc = load_library().kv8_store(cache._segments, len(cache.segments), begin, end, k.data_ptr(), v.data_ptr(), dt, _layout(k), B, H, 64,
                                   _check_lens(lens, B, device), k8, k_scale, v8, v_scale, _raw_stream(device.index))
     if rc != 0:
         _check(rc)
@@ -657,8 +662,8 @@ def litevar_windowed_attn_kv8_fwd(plan, q, cache, sm_scale, out=None, cfg_share=
     assert out.shape == shape and out.dtype == q.dtype and out.device == device
     keep, work_ptr, work_bytes = _workspace(workspace, lambda: litevar_windowed_attn_kv8_workspace_bytes(plan, B, H), device)
     k8, k_scale, v8, v_scale = cache._pointers()
-    rc = load_library().attn_kv8_fwd(C.addressof(handle), q.data_ptr(), k8, k_scale, v8, v_scale, out.data_ptr(), B, H, D, _strides(q),
-                                     _strides(out), sm_scale, share_ptr, flags, work_ptr, work_bytes,
+    rc = load_library().attn_kv8_fwd(C.addressof(handle), q.data_ptr(), k8, k_scale, v8, v_scale, out.data_ptr(), B, H, D, _layout(q),
+                                     _layout(out), sm_scale, share_ptr, flags, work_ptr, work_bytes,
                                      _raw_stream(device.index))
     if rc != 0:
         _check(rc)
@@ -695,7 +700,7 @@ def litevar_cross_attn_fwd(q, k, v, sm_scale, lens=None, out=None, workspace=Non
     assert out.shape == shape and out.dtype == dtype and out.device == device
     keep, work_ptr, work_bytes = _workspace(workspace, lambda: litevar_cross_attn_workspace_bytes(B, H, H_kv, q_len, kv_len), device)
     rc = load_library().cross_attn_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), B, H, H_kv, q_len, kv_len, D, dt,
-                                       _strides(q), _strides(k), _strides(out), _check_lens(lens, B, device), sm_scale, work_ptr,
+                                       _layout(q), _layout(k), _layout(out), _check_lens(lens, B, device), sm_scale, work_ptr,
                                        work_bytes, _raw_stream(device.index))
     if rc != 0:
         _check(rc)
@@ -722,7 +727,7 @@ def litevar_cross_attn_kv8_fwd(q, cache, sm_scale, lens=None, out=None, workspac
     keep, work_ptr, work_bytes = _workspace(workspace, lambda: litevar_cross_attn_workspace_bytes(B, H, H_kv, q_len, kv_len), device)
     k8, k_scale, v8, v_scale = cache._pointers()
     rc = load_library().cross_attn_kv8_fwd(q.data_ptr(), k8, k_scale, v8, v_scale, out.data_ptr(), B, H, H_kv, q_len, kv_len, D,
-                                           _strides(q), _strides(out), _check_lens(lens, B, device), sm_scale, work_ptr, work_bytes,
+                                           _layout(q), _layout(out), _check_lens(lens, B, device), sm_scale, work_ptr, work_bytes,
                                            _raw_stream(device.index))
     if rc != 0:
         _check(rc)
