@@ -408,6 +408,48 @@ __device__ inline void row_again(const CrossArgs& a, float c, int b, int j, int 
   ((T*)a.o + b * a.os[0] + qr.h * a.os[1] + qr.i * a.os[2])[lane] = (T)(o * (1.f / l));
 }
 
+// A wave's 32 rows from row0 on: O times unit over the row sum, of which `part` is this lane's share (no key: zeros), as
+// bf16.  Rows whose reference went too far (their lanes in `far`), and rows whose products with V overflowed under a sum that
+// had been let grow (the reference has moved, or the sum is above one per key), are formed again behind the store.
+template <int KIND>
+__device__ inline void store_tile(const CrossArgs& a, float c, int b, int j, int bj, int n_keys, int row0, const f32x16 (&O)[2],
+                                  float part, float unit, uint64_t far, uint64_t moved) {
+  const float l = part + other_half(part), inv = l > 0.f ? 1.f / l : 0.f;
+  unsigned r[2][8];
+#pragma unroll
+  for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) {
+      float x = O[dt][e] * inv, y = O[dt][e + 1] * inv;
+      if constexpr (KIND == kCodes) { x *= unit; y *= unit; }
+      r[dt][e / 2] = __builtin_bit_cast(unsigned, bf16x2{(__bf16)x, (__bf16)y});
+    }
+  const int row = row0 + (lane_of_wave() & 31);          // (formed anew: not worth registers through the loop)
+  if (row < a.rows) {
+    const Row qr = row_at(a, j, row);
+    __bf16* op = (__bf16*)a.o + b * a.os[0] + qr.h * a.os[1] + qr.i * a.os[2] + 8 * (lane_of_wave() >> 5);
+#pragma unroll
+    for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) {
+        // dims 32 dt + 16 jj .. + 15 of the row: its lanes hold 4 of each 8; exchanged, 8 in a row
+        const auto x0 = __builtin_amdgcn_permlane32_swap(r[dt][4 * jj], r[dt][4 * jj + 2], false, false);
+        const auto x1 = __builtin_amdgcn_permlane32_swap(r[dt][4 * jj + 1], r[dt][4 * jj + 3], false, false);
+        const u32x4 piece = {x0[0], x1[0], x0[1], x1[1]};
+        *(u32x4*)(op + 32 * dt + 16 * jj) = piece;
+      }
+  }
+  const uint64_t again = (far | moved | __builtin_amdgcn_ballot_w64(l > (float)n_keys)) & __builtin_amdgcn_ballot_w64(row < a.rows);
+  if (__builtin_expect(again != 0, 0)) {
+    float any = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) any = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, r[e >> 3][e & 7]), kOnes, any, false);
+    uint64_t bad = (far | __builtin_amdgcn_ballot_w64(not_finite(any))) & again;
+    bad = (bad | (bad >> 32)) & 0xffffffffull;
+    for (; bad != 0; bad &= bad - 1) row_again<KIND>(a, c, b, j, bj, n_keys, row0 + __builtin_ctzll(bad));
+  }
+}
+
 // Many rows: NWV waves of one (batch, kv head), each with 32 rows, share the K and V rows, which pass through LDS in chunks
 // of 64 keys, three buffers: one read, one landing, one whose last readers may be behind, so that one barrier per chunk
 // is enough.  bf16 rows come by LDS-DMA; codes through registers, converted (exactly) on their way, one chunk ahead.  The
@@ -420,6 +462,11 @@ __device__ inline void row_again(const CrossArgs& a, float c, int b, int j, int 
 // Codes: a chunk is a block, its K scale joins the softmax scale.  Its V scale, relative to the largest of the
 // keys that count, is added to the exponent, which costs nothing per score; the chunk's part of the row sum is divided by it
 // again.  (Relative V scales are taken as at least 2^-96, so that no probability that counts is flushed to zero.)
+//
+// 288 pairs of 2240 rows on 149 to 512 keys: 88 us (650 TFLOP/s; on 2048 keys each 870).  What bounds it there is the vector issue,
+// 54 instructions and 16 exponentials for 32 rows x 32 keys, about 300 more for a tile's start and end, and Q and O, 34 us
+// at the copy rate, beside which a round of workgroups starts and ends with little else to do.  512 workgroups that stay, each with
+// a run of five or six tiles whose rows of Q come under the tile before: 102 us (the runs are uneven).
 template <int NWV, int KIND>
 __global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(NWV == 4 ? 3 : 4, NWV == 4 ? 3 : 4)))
 void k_cross_tiles(CrossArgs a, float c) {
@@ -514,7 +561,7 @@ void k_cross_tiles(CrossArgs a, float c) {
   f32x16 O[2] = {f32x16{}, f32x16{}};
   float L[2] = {0.f, 0.f}, negm = 0.f;         // this lane's part of the row sum, one chain per slice; minus the reference (base 2)
   bool unset = true;
-  uint64_t far = 0;                            // lanes whose reference has been beyond kFar
+  uint64_t far = 0, moved = 0;                 // lanes whose reference has been beyond kFar, has moved
 
   auto is_beyond = [](float x) { return __builtin_amdgcn_ballot_w64(!(fabsf(x) < (CODES ? kFarCodes : kFarReference))); };
   auto scores = [&](u32x4 (&kr)[4]) -> f32x16 {
@@ -574,6 +621,7 @@ void k_cross_tiles(CrossArgs a, float c) {
       const float shift = now > kMostSum ? rintf(to) : 0.f, alpha = __builtin_amdgcn_exp2f(-shift);
       negm -= shift; L[0] *= alpha; L[1] *= alpha;
       far |= is_beyond(negm);
+      moved |= __builtin_amdgcn_ballot_w64(shift != 0.f);
 #pragma unroll
       for (int e = 0; e < 16; ++e) { O[0][e] *= alpha; O[1][e] *= alpha; }
       exponentials();
@@ -672,39 +720,7 @@ void k_cross_tiles(CrossArgs a, float c) {
     }
   }
 
-  if (!working) return;
-  const float part = L[0] + L[1], l = part + other_half(part), inv = l > 0.f ? 1.f / l : 0.f, unit = CODES ? vmax : 1.f;   // (no key: zeros)
-  unsigned r[2][8];
-#pragma unroll
-  for (int dt = 0; dt < 2; ++dt)
-#pragma unroll
-    for (int e = 0; e < 16; e += 2) {
-      float x = O[dt][e] * inv, y = O[dt][e + 1] * inv;
-      if constexpr (CODES) { x *= unit; y *= unit; }
-      r[dt][e / 2] = __builtin_bit_cast(unsigned, bf16x2{(__bf16)x, (__bf16)y});
-    }
-  float any = 0.f;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) any = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, r[e >> 3][e & 7]), kOnes, any, false);
-  int row = row0 + (lane_of_wave() & 31);      // (formed anew: not worth registers through the loop)
-  if (row < a.rows) {
-    const Row qr = row_at(a, j, row);
-    __bf16* op = (__bf16*)a.o + b * a.os[0] + qr.h * a.os[1] + qr.i * a.os[2] + 8 * (lane_of_wave() >> 5);
-#pragma unroll
-    for (int dt = 0; dt < 2; ++dt)
-#pragma unroll
-      for (int jj = 0; jj < 2; ++jj) {
-        // dims 32 dt + 16 jj .. + 15 of the row: its lanes hold 4 of each 8; exchanged, 8 in a row
-        const auto x0 = __builtin_amdgcn_permlane32_swap(r[dt][4 * jj], r[dt][4 * jj + 2], false, false);
-        const auto x1 = __builtin_amdgcn_permlane32_swap(r[dt][4 * jj + 1], r[dt][4 * jj + 3], false, false);
-        const u32x4 piece = {x0[0], x1[0], x0[1], x1[1]};
-        *(u32x4*)(op + 32 * dt + 16 * jj) = piece;
-      }
-  }
-  // Rows whose reference went too far, and rows whose products with V overflowed under a sum that had been let grow.
-  uint64_t bad = (far | __builtin_amdgcn_ballot_w64(not_finite(any))) & __builtin_amdgcn_ballot_w64(row < a.rows);
-  bad = (bad | (bad >> 32)) & 0xffffffffull;
-  for (; __builtin_expect(bad != 0, 0); bad &= bad - 1) row_again<KIND>(a, c, b, j, bj, n_keys, row0 + __builtin_ctzll(bad));
+  if (working) store_tile<KIND>(a, c, b, j, bj, n_keys, row0, O, L[0] + L[1], CODES ? vmax : 1.f, far, moved);
 }
 
 // a lane's half of a K row of 256 bytes, eight pieces; issued only, a wait must precede the first use

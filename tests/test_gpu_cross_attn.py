@@ -79,9 +79,12 @@ SHAPES = [  # B, H, H_kv, q_len, kv_len
     (2, 3, 3, 7, 0), (2, 3, 3, 0, 7),
     # rows that share K and V through LDS, in four and in eight waves; with shared heads
     (8, 32, 32, 257, 200), (16, 32, 32, 100, 77), (16, 32, 8, 140, 130), (8, 64, 64, 300, 33), (4, 64, 64, 1000, 1), (16, 32, 32, 130, 0),
+    (8, 64, 64, 530, 130), (16, 32, 32, 700, 65), (31, 34, 17, 300, 97),
 ]
 # (rows of a call that share K and V through LDS, whatever the type: 2560 tiles)
 MANY = (16, 32, 130)
+# (and in workgroups of eight waves, more of them than the chip holds)
+MORE = (16, 32, 520)
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "codes"])
@@ -97,7 +100,7 @@ def test_cross_attention(lv, shape, ragged, kind):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "codes"])
-@pytest.mark.parametrize("B,H,n", [(6, 3, 40), MANY], ids=str)
+@pytest.mark.parametrize("B,H,n", [(6, 3, 40), MANY, MORE], ids=str)
 def test_rows_behind_the_length_are_not_read(lv, kind, B, H, n):
     L = 150
     lens = torch.tensor(([150, 1, 64, 65, 0, 97] + list(range(20, 40)))[:B], dtype=torch.int32).cuda()
@@ -121,7 +124,7 @@ def test_lengths_outside_the_axis_are_taken_as_its_ends(lv, n):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
-@pytest.mark.parametrize("H,n", [(4, 1), (4, 50), (4, 300), (150, 141)])
+@pytest.mark.parametrize("H,n", [(4, 1), (4, 50), (4, 300), (150, 141), (160, 600)])
 def test_strides(lv, kind, H, n):
     """Rows as a fused projection leaves them, K and V of one prompt shared by the batch, an output inside a larger one."""
     B, L = 3, 90
@@ -138,7 +141,7 @@ def test_strides(lv, kind, H, n):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "codes"])
-@pytest.mark.parametrize("B,H,n", [(2, 2, 2), (2, 2, 130), MANY], ids=str)
+@pytest.mark.parametrize("B,H,n", [(2, 2, 2), (2, 2, 130), MANY, MORE], ids=str)
 def test_peaked_and_far_scores(lv, kind, B, H, n):
     """Scores of many sizes: one key takes nearly everything, scores fall and rise along the axis."""
     L = 300
@@ -152,7 +155,7 @@ def test_peaked_and_far_scores(lv, kind, B, H, n):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "codes"])
-@pytest.mark.parametrize("B,H,n", [(1, 1, 1), (1, 1, 100), MANY], ids=str)
+@pytest.mark.parametrize("B,H,n", [(1, 1, 1), (1, 1, 100), MANY, MORE], ids=str)
 def test_scores_that_fp32_holds_keep_their_differences(lv, kind, B, H, n):
     """Scores around 2^27 whose differences are whole numbers of 2^20: the largest keys win, exactly."""
     L = 128
@@ -169,7 +172,7 @@ def test_scores_that_fp32_holds_keep_their_differences(lv, kind, B, H, n):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
-@pytest.mark.parametrize("B,H,n", [(1, 2, 40), MANY], ids=str)
+@pytest.mark.parametrize("B,H,n", [(1, 2, 40), MANY, MORE], ids=str)
 def test_values_near_the_end_of_the_range(lv, kind, B, H, n):
     """Values of 2^120 and scores that rise along the axis: sums under a reference that moves do not overflow into the
     result."""
@@ -197,7 +200,7 @@ def test_blocks_of_very_different_scales(lv):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "codes"])
-@pytest.mark.parametrize("shape", [(2, 4, 4, 3, 5000), (2, 4, 4, 200, 300), (16, 32, 32, 130, 70)], ids=str)
+@pytest.mark.parametrize("shape", [(2, 4, 4, 3, 5000), (2, 4, 4, 200, 300), (16, 32, 32, 130, 70), (16, 32, 32, 520, 70)], ids=str)
 def test_workspace_contents_do_not_matter_and_runs_repeat(lv, kind, shape):
     B, H, Hkv, n, L = shape
     need = lv.litevar_cross_attn_workspace_bytes(B, H, Hkv, n, L)
@@ -225,7 +228,7 @@ def test_offsets_beyond_32_bits(lv):
         plain.assert_close(out, want, _tolerance("bf16", want, A, S, L))
 
 
-@pytest.mark.parametrize("H,n,L", [(4, 2, 6000), (4, 150, 300), (300, 130, 100)])
+@pytest.mark.parametrize("H,n,L", [(4, 2, 6000), (4, 150, 300), (300, 130, 100), (300, 520, 100)])
 def test_streams_and_graphs(lv, H, n, L):
     B = 2
     side = torch.cuda.Stream()
