@@ -1016,7 +1016,8 @@ template <int KIND> litevar_status launch(CrossArgs& a, float c, hipStream_t st)
   if (shares_rows<KIND>(a)) {
     // Eight waves to a workgroup read K and V half as often; four waste less on few tiles and leave less of the chip idle:
     // (tiles of a pair, pairs), 1024 keys, eight / four: (8, 64) 21.4 / 18.2; (22, 64) 23.0 / 25.2; (8, 256) 25.9 / 27.8; (22, 480) 106 / 118.
-    // On codes eight spill registers: (8, 480) 53.0 / 54.1, (8, 256) 33.8 / 31.8.
+    // On codes eight spill registers, (8, 480) 53.0 / 54.1, (8, 256) 33.8 / 31.8, and of workgroups of six a CU holds one: (6, 480),
+    // 256 keys, six / four 22.9 / 21.0, (8, 480) 39.2 / 22.0.
     const int nwv = KIND == kBf16 && a.tiles > 4 && (int64_t)a.B * a.Hkv * ((a.tiles + 7) / 8) >= 192 ? 8 : 4;
     const int64_t pairs = (int64_t)a.B * a.Hkv;
     a.groups = (a.tiles + nwv - 1) / nwv; a.groups_magic = magic_of(a.groups);
