@@ -222,3 +222,63 @@ def test_softmax_scales(lv, sm):
         out = lv.litevar_windowed_attn_kv8_fwd(plan, q, cache, sm)
         want, A, S, floor = _reference(cache, q, lv.litevar_mask_export_dense(plan)[0].bool(), sm)
         plain.assert_close(out, want, _tolerance(A, S, floor))
+
+
+@pytest.mark.parametrize("route", ROUTES, ids=str)
+def test_bounds_checking_build_finds_nothing(lv, route):
+    from paper_2411_17178_amd import build as hip_build
+    q_scales, waves = route
+    B, H = 2, 3
+    plan = lv.litevar_mask_build(VAR256, 3, None, 0, q_scales, waves_per_group=waves)
+    cache = _cache(lv, VAR256, B, H, 9)
+    q = torch.randn(B, H, plan.q_len, 64, device="cuda").to(torch.bfloat16)
+    out = lv.litevar_windowed_attn_kv8_fwd(plan, q, cache, SM)
+    with lv.use_library(hip_build.LIB_DEBUG_BOUNDS):
+        checked = lv.litevar_windowed_attn_kv8_fwd(plan, q, cache, SM)
+    lv.litevar_plan_check(plan)
+    assert torch.equal(out, checked)
+
+
+def test_calls_on_two_streams(lv):
+    """Calls that run beside each other, each with what it allocates itself."""
+    B, H = 4, 16
+    plans = [lv.litevar_mask_build(VAR256, 3, None, 0, q_scales, waves_per_group=waves) for q_scales, waves in ROUTES]
+    cache = _cache(lv, VAR256, B, H, 10)
+    qs = [torch.randn(B, H, p.q_len, 64, device="cuda").to(torch.bfloat16) for p in plans]
+    want = [lv.litevar_windowed_attn_kv8_fwd(p, q, cache, SM) for p, q in zip(plans, qs)]
+    streams = [torch.cuda.Stream() for _ in plans]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [[lv.litevar_windowed_attn_kv8_fwd(p, q, cache, SM, stream=s) for p, q, s in zip(plans, qs, streams)] for _ in range(5)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for outs in got for a, b in zip(outs, want))
+
+
+def test_the_binding_refuses_what_does_not_fit(lv):
+    B, H = 2, 3
+    plan = lv.litevar_mask_build(VAR256, 3, None, 0, (9, 10))
+    cache = _cache(lv, VAR256, B, H, 11)
+    q = torch.zeros(B, H, 256, 64, dtype=torch.bfloat16, device="cuda")
+    other = lv.litevar_kv8_cache([s * s for s in (1, 2, 3, 4, 5, 6, 8, 10, 16, 13)], B, H)
+    for bad in (other, lv.litevar_kv8_cache([680], B, H), lv.litevar_kv8_cache([s * s for s in VAR256], B, H + 1)):
+        with pytest.raises(AssertionError):
+            lv.litevar_windowed_attn_kv8_fwd(plan, q, bad, SM)
+    with pytest.raises(TypeError):
+        lv.litevar_windowed_attn_kv8_fwd(plan, q.float(), cache, SM)
+    with pytest.raises(AssertionError):
+        lv.litevar_cross_attn_kv8_fwd(q, cache, SM)
+    full = lv.litevar_mask_build(VAR256, 2, waves_per_group=16)
+    need = lv.litevar_windowed_attn_kv8_workspace_bytes(full, B, H)
+    assert need == B * H * 680 * 256
+    with pytest.raises(lv.LitevarError):
+        lv.litevar_windowed_attn_kv8_fwd(full, torch.zeros(B, H, 680, 64, dtype=torch.bfloat16, device="cuda"), cache, SM,
+                                         workspace=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(lv.LitevarError):
+        lv.litevar_windowed_attn_kv8_fwd(plan, q, cache, -1.0)
+    k = torch.zeros(B, H, 4, 64, dtype=torch.bfloat16, device="cuda")
+    for args, kw in (((cache, k, k, (2, 3)), {}), ((cache, k, k, (1, 2)), dict(lens=torch.zeros(B, dtype=torch.int64, device="cuda"))),
+                     ((cache, k, k[:, :, :3], (1, 2)), {}), ((cache, k, k, (9, 11)), {})):
+        with pytest.raises(AssertionError):
+            lv.litevar_kv8_store(*args, **kw)
+    with pytest.raises(TypeError):
+        lv.litevar_kv8_store(cache, k.half(), k.half(), (1, 2))
