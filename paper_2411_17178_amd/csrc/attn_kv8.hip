@@ -13,6 +13,10 @@
 // Nothing of K or V is shared between waves or goes through LDS; the step's 32 pairs of scales do (a lane looks up one
 // key, every lane reads the eight it owns).  Scales that are not finite reach the queries that keep their keys only:
 // nothing is multiplied with a scale where the probability is zero.
+//
+// Bound: start-up (descriptor, tokens, rows, products one behind the other).  16 queries, 480 pairs 5.0 us in a graph; 25 queries
+// 7.7 with one wave per patch, 10.1 with four.  Not for longer steps: 256 queries on 680 keys 80 us, 30 with keys shared
+// through LDS.
 #include "attn_bf16_common.h"
 
 namespace lv {
