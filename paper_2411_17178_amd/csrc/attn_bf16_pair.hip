@@ -138,7 +138,7 @@ __device__ inline f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) { return __builtin_a
 __device__ inline f16x8 codes_to_f16(unsigned lo, unsigned hi, float s) {
   f16x8 r;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = (_Float16)(s * (float)(int8_t)(((e < 4 ? lo : hi) >> (8 * (e & 3))) & 0xffu));
+  for (int e = 0; e < 8; ++e) r[e] = (_Float16)(s * (float)((int)((e < 4 ? lo : hi) << (24 - 8 * (e & 3))) >> 24));
   return r;
 }
 

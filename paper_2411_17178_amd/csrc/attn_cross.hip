@@ -12,7 +12,8 @@
 // What a call cannot do without: Q, O and the valid keys' K and V once, 256 operations per row and key.  256 rows, 480 pairs of 77 to 512
 // keys, bf16: 22.9 us for 73 MB (14.4 at the copy rate); 2240 rows, 32 pairs, fp32: 56 us for 4.2 TFLOP (27 at a large
 // product's rate); four rows (one token, 4 query
-// heads) on up to 30 011 keys in codes, 16 pairs: 18.5 us for 44 MB (8.7).
+// heads) on up to 30 011 keys in codes, 16 pairs: 17.7 us for 44 MB (8.7); 169 rows, 480 pairs of 51 to 333
+// keys in codes: 18.1 us (7.0).
 #include <cmath>
 #include <cstring>
 #include <type_traits>
@@ -65,7 +66,7 @@ __device__ inline float uniform(float x) { return __uint_as_float(__builtin_amdg
 __device__ inline bf16x8 codes_to_bf16(unsigned lo, unsigned hi) {
   bf16x8 r;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = (__bf16)(float)(int8_t)(((e < 4 ? lo : hi) >> (8 * (e & 3))) & 0xffu);
+  for (int e = 0; e < 8; ++e) r[e] = (__bf16)(float)((int)((e < 4 ? lo : hi) << (24 - 8 * (e & 3))) >> 24);
   return r;
 }
 
@@ -459,14 +460,19 @@ __device__ inline void store_tile(const CrossArgs& a, float c, int b, int j, int
 
 // Many rows: NWV waves of one (batch, kv head), each with 32 rows, share the K and V rows, which pass through LDS in chunks
 // of 64 keys, three buffers: one read, one landing, one whose last readers may be behind, so that one barrier per chunk
-// is enough.  bf16 rows come by LDS-DMA; codes through registers, converted (exactly) on their way, one chunk ahead.  The
-// score products of a block of 32 keys are issued ahead of the exponentials of the block before it.
+// is enough.  All come by LDS-DMA.  The score products of a block of 32 keys are issued ahead of the exponentials of the
+// block before it.
 //
 // Softmax in base 2: the reference is the largest score of the first block and moves (by whole powers of two) when a sum
 // passes 2^40, so that no maximum is formed in the other blocks.  Rows whose reference went beyond kFarReference, where its
 // rounding would show, and rows that overflowed are formed again behind the store.
 //
-// Codes: a chunk is a block, its K scale joins the softmax scale.  Its V scale, relative to the largest of the
+// Codes come to a place behind the buffers and are converted (exactly) from there by the wave that brought them.  Two buffers
+// do, 40 KiB with the codes, so that a CU holds four workgroups of four waves or two of eight; it costs the score products
+// issued ahead across chunks.  480 pairs of 169 rows on 384 keys: three buffers, codes through registers, workgroups of four
+// 24.5 us; three chunks of codes on their way instead of one 24.3 (nothing waits for memory); so 23.8; of eight, which convert a
+// chunk once for six tiles, and a byte in one instruction, 21.0 (18.0 in bf16).
+// A chunk is a block, its K scale joins the softmax scale.  Its V scale, relative to the largest of the
 // keys that count, is added to the exponent, which costs nothing per score; the chunk's part of the row sum is divided by it
 // again.  (Relative V scales are taken as at least 2^-96, so that no probability that counts is flushed to zero.)
 //
@@ -475,11 +481,11 @@ __device__ inline void store_tile(const CrossArgs& a, float c, int b, int j, int
 // at the copy rate, beside which a round of workgroups starts and ends with little else to do.  512 workgroups that stay, each with
 // a run of five or six tiles whose rows of Q come under the tile before: 102 us (the runs are uneven).
 template <int NWV, int KIND>
-__global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(NWV == 4 ? 3 : 4, NWV == 4 ? 3 : 4)))
+__global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(NWV == 4 && KIND == kBf16 ? 3 : 4, NWV == 4 && KIND == kBf16 ? 3 : 4)))
 void k_cross_tiles(CrossArgs a, float c) {
   constexpr bool CODES = KIND == kCodes;
   constexpr int kRowsPerWave = kBlock / NWV, kTransfers = kRowsPerWave / 8, kBuf = 2 * kBlock * kRow;
-  __shared__ __align__(1024) unsigned char smem[3 * kBuf];
+  __shared__ __align__(1024) unsigned char smem[CODES ? 2 * kBuf + 8192 : 3 * kBuf];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int n = lane & 31, hh = lane >> 5;
   // Workgroup i runs on XCD i % 8, each with an L2 of its own: the tiles of a pair follow one another on one XCD, or, with
@@ -524,33 +530,50 @@ void k_cross_tiles(CrossArgs a, float c) {
       __builtin_amdgcn_global_load_lds((global_void*)((const unsigned char*)a.v + base + src), (lds_void*)(dst + kBlock * kRow), 16, 0, 0);
     }
   };
-  // codes: 16 of a K or V row per thread and piece, 512 pieces to a chunk
-  constexpr int kPieces = 512 / (NWV * 64);
-  [[maybe_unused]] u32x4 codes[kPieces];
-  [[maybe_unused]] auto load_chunk = [&](int chunk) {
+  // codes: a chunk is eight pieces of 16 K or V rows, 1 KiB each, which LDS-DMA leaves behind the buffers; the wave that
+  // brought a piece converts it into a buffer
+  constexpr int kPieces = 8 / NWV;
+  [[maybe_unused]] unsigned char* const stage = smem + 2 * kBuf;
+  [[maybe_unused]] auto issue_codes = [&](int chunk) {
+    int lane = lane_of_wave();
+    asm volatile("" : "+v"(lane));             // (addresses formed anew in every chunk: not worth registers through the loop)
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int at = tid + NWV * 64 * i, key = min((at & 255) >> 2, n_keys - 1 - kBlock * chunk);
-      const int8_t* base = (const int8_t*)(wave + NWV * i < 4 ? a.k : a.v) + kv_at + (int64_t)chunk * (kBlock * 64);
-      codes[i] = *(const u32x4*)(base + (unsigned)(key * 64 + 16 * (at & 3)));
+      const int piece = wave + NWV * i, key = min(16 * (piece & 3) + (lane >> 2), n_keys - 1 - kBlock * chunk);
+      const int8_t* base = (const int8_t*)(piece < 4 ? a.k : a.v) + kv_at + (int64_t)chunk * (kBlock * 64);
+      __builtin_amdgcn_global_load_lds((global_void*)(base + (unsigned)(key * 64 + 16 * (lane & 3))), (lds_void*)(stage + 1024 * piece), 16, 0, 0);
     }
   };
-  [[maybe_unused]] auto commit_chunk = [&](int buf) {
+  [[maybe_unused]] auto commit_codes = [&](int buf_at) {
+    int lane = lane_of_wave();
+    asm volatile("" : "+v"(lane));
+    wait_vmcnt<0>();
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int at = tid + NWV * 64 * i, row = (at & 255) >> 2;
-      const unsigned p = 2u * ((unsigned)at & 3u), sw = dense_swizzle((unsigned)row);
-      unsigned char* dst = smem + buf * kBuf + (at < 256 ? 0 : kBlock * kRow) + row * kRow;
-      *(bf16x8*)(dst + ((p ^ sw) << 4)) = codes_to_bf16(codes[i][0], codes[i][1]);
-      *(bf16x8*)(dst + (((p + 1u) ^ sw) << 4)) = codes_to_bf16(codes[i][2], codes[i][3]);
+      const int piece = wave + NWV * i, row = 16 * (piece & 3) + (lane >> 2);
+      const u32x4 codes = *(const u32x4*)(stage + 1024 * piece + 16 * lane);
+      const unsigned at = 2u * ((unsigned)lane & 3u), sw = dense_swizzle((unsigned)row);
+      unsigned char* dst = smem + buf_at + (piece < 4 ? 0 : kBlock * kRow) + row * kRow;
+      *(bf16x8*)(dst + ((at ^ sw) << 4)) = codes_to_bf16(codes[0], codes[1]);
+      *(bf16x8*)(dst + (((at + 1u) ^ sw) << 4)) = codes_to_bf16(codes[2], codes[3]);
     }
   };
-  // a chunk's scales, as scalar loads (requested half a chunk ahead), and log2 of the largest V scale
-  [[maybe_unused]] float vmax = 0.f, log_vmax = 0.f;
-  [[maybe_unused]] int ks_bits = 0, vs_bits = 0;
-  [[maybe_unused]] auto load_scales = [&](int chunk) {
-    const int64_t at = (int64_t)bj * a.scale_blocks + chunk;
-    ks_bits = ((const_i32_ptr)a.k_scale)[at]; vs_bits = ((const_i32_ptr)a.v_scale)[at];
+  // the scales of 64 chunks, one to a lane: K's, log2 of V's relative to the largest and its reciprocal
+  [[maybe_unused]] float vmax = 0.f, log_vmax = 0.f, lane_ks = 1.f, lane_lv = 0.f, lane_iv = 1.f;
+  [[maybe_unused]] auto scales_at = [&](int chunk) {
+    int lane = lane_of_wave();
+    asm volatile("" : "+v"(lane));             // (formed anew: not worth a register through the loop)
+    return (int64_t)bj * a.scale_blocks + min(chunk + lane, n_chunks - 1);
+  };
+  [[maybe_unused]] auto set_scales = [&](float ks, float vs) {
+    lane_ks = ks;
+    // (a scale of zero belongs to a block of zeros: any will do)
+    lane_lv = vs > 0.f ? fmaxf(__builtin_amdgcn_logf(vs) - log_vmax, -96.f) : 0.f;
+    lane_iv = __builtin_amdgcn_exp2f(-lane_lv);
+    asm volatile("" : "+v"(lane_ks));          // (its load is waited for here, not wherever the chunks go on)
+  };
+  [[maybe_unused]] auto scale_of = [](float x, int chunk) {
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), chunk & 63));
   };
 
   // LDS read offsets: K piece 2 t + hh of row n; V: 4 keys x 16 dims per 16 lanes
@@ -579,13 +602,16 @@ void k_cross_tiles(CrossArgs a, float c) {
       S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[t]), qf[t], S, 0, 0, 0);
     return S;
   };
-  // the rest of a block, its V rows requested; ks, lv, iv: of its chunk
-  auto absorb = [&](f32x16& S, u32x2 (&va)[8], int key0, float ks, float lv, float iv) {
+  // of the block from key0 on, the scores of keys that do not exist
+  auto mask = [&](f32x16& S, int key0) {
     if (key0 + 32 > n_keys) {                  // (uniform)
       const int left = n_keys - key0 - 4 * hh;
 #pragma unroll
       for (int e = 0; e < 16; ++e) S[e] = 8 * (e >> 2) + (e & 3) < left ? S[e] : -INFINITY;
     }
+  };
+  // the rest of a block, its V rows requested; ks, lv, iv: of its chunk
+  auto absorb = [&](f32x16& S, u32x2 (&va)[8], float ks, float lv, float iv) {
     if (CODES && ks < 0x1p-100f) {             // (a block of zeros or nearly so: scaled here, c ks would lose its bits)
 #pragma unroll
       for (int e = 0; e < 16; ++e) S[e] = S[e] > -INFINITY ? S[e] * ks : S[e];
@@ -646,84 +672,120 @@ void k_cross_tiles(CrossArgs a, float c) {
 
   if (n_chunks > 0) {
     if constexpr (CODES) {
-      load_chunk(0);
-      for (int at = 0; at < n_chunks; at += 64) vmax = fmaxf(vmax, a.v_scale[(int64_t)bj * a.scale_blocks + min(at + lane, n_chunks - 1)]);
-#pragma unroll
-      for (int d = 32; d > 0; d >>= 1) vmax = fmaxf(vmax, __shfl_xor(vmax, d));
-      vmax = uniform(vmax);
+      const float ks = a.k_scale[scales_at(0)], vs = a.v_scale[scales_at(0)];
+      issue_codes(0);
+      vmax = vs;
+      for (int at = 64; at < n_chunks; at += 64) vmax = fmaxf(vmax, a.v_scale[scales_at(at)]);
+      vmax = wave_max(vmax);
       log_vmax = uniform(__builtin_amdgcn_logf(vmax));
-      load_scales(0);
-      commit_chunk(0);
-      if (n_chunks > 1) load_chunk(1);
-      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      set_scales(ks, vs);
+      commit_codes(0);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (n_chunks > 1) issue_codes(1);
+      asm volatile("s_barrier" ::: "memory");
     } else {
       issue_chunk(0, 0);
       if (n_chunks > 1) { issue_chunk(1, 1); wait_vmcnt<2 * kTransfers>(); } else wait_vmcnt<0>();
       asm volatile("" : "+v"(qf[0]), "+v"(qf[1]), "+v"(qf[2]), "+v"(qf[3]));   // (older than the chunks: in)
       asm volatile("s_barrier" ::: "memory");
     }
-    f32x16 S0 = f32x16{};                      // scores of the chunk's first block
-    if (working) {
-      u32x4 kr[4];
-      read_k<0>(k_off, kr);
-      S0 = scores(kr);
-    }
-    // A chunk: its two blocks, each with the next block's score products in front of its own exponentials.  Between the
-    // blocks the next chunk is made sure of and the one after it requested, for the buffer that every wave has read to
-    // its end by then.
-    auto one = [&](int chunk, auto which) -> bool {
-      constexpr int p = decltype(which)::value, AT = p * kBuf, NEXT = (p + 1) % 3 * kBuf;
-      const int key0 = chunk * kBlock;
-      const bool more = chunk + 1 < n_chunks, second = key0 + 32 < n_keys;
-      float ks = 1.f, lv = 0.f, iv = 1.f;
-      if constexpr (CODES) {
-        // (a scale of zero belongs to a block of zeros: any will do)
-        ks = __int_as_float(ks_bits);
-        lv = uniform(__int_as_float(vs_bits) > 0.f ? fmaxf(__builtin_amdgcn_logf(__int_as_float(vs_bits)) - log_vmax, -96.f) : 0.f);
-        iv = uniform(__builtin_amdgcn_exp2f(-lv));
-      }
-      f32x16 S1;
-      asm volatile("" : "=v"(S1));             // (not set where there is no second block, and not used then)
-      if (working) {
-        u32x2 va[8];
-        if (second) {
-          u32x4 kr[4];
-          read_k<AT + 32 * kRow>(k_off, kr);
-          S1 = scores(kr);
+    if constexpr (CODES) {
+      // A chunk: the score products of both blocks, then their exponentials.  In between the next chunk is converted into
+      // the other buffer, which nobody has read since the barrier that let this chunk begin.
+      for (int chunk = 0, at = 0;; ++chunk, at = kBuf - at) {
+        const float ks = scale_of(lane_ks, chunk), lv = scale_of(lane_lv, chunk), iv = scale_of(lane_iv, chunk);
+        const int key0 = chunk * kBlock;
+        const bool more = chunk + 1 < n_chunks, second = key0 + 32 < n_keys;
+        const unsigned v_at[2] = {v_off[0] + at, v_off[1] + at};
+        f32x16 S1;
+        asm volatile("" : "=v"(S1));             // (not set where there is no second block, and not used then)
+        if (working) {
+          const unsigned k_at[4] = {k_off[0] + at, k_off[1] + at, k_off[2] + at, k_off[3] + at};
+          f32x16 S0;
+          u32x2 va[8];
+          {
+            u32x4 kr[4];
+            read_k<0>(k_at, kr);
+            S0 = scores(kr);
+          }
+          if (second) {
+            u32x4 kr[4];
+            read_k<32 * kRow>(k_at, kr);
+            S1 = scores(kr);
+          }
+          read_v<kBlock * kRow>(v_at, va);
+          __builtin_amdgcn_sched_barrier(0);
+          mask(S0, key0);
+          absorb(S0, va, ks, lv, iv);
         }
-        read_v<AT + kBlock * kRow>(v_off, va);
-        __builtin_amdgcn_sched_barrier(0);
-        absorb(S0, va, key0, ks, lv, iv);
+        if (more) {
+          commit_codes(kBuf - at);
+          if (((chunk + 1) & 63) == 0) set_scales(a.k_scale[scales_at(chunk + 1)], a.v_scale[scales_at(chunk + 1)]);
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          if (chunk + 2 < n_chunks) issue_codes(chunk + 2);
+        }
+        if (working && second) {
+          u32x2 va[8];
+          read_v<(kBlock + 32) * kRow>(v_at, va);
+          __builtin_amdgcn_sched_barrier(0);
+          mask(S1, key0 + 32);
+          absorb(S1, va, ks, lv, iv);
+        }
+        if (!more) break;
+        asm volatile("s_barrier" ::: "memory");
       }
-      if (more) {
-        if constexpr (CODES) {
-          commit_chunk((p + 1) % 3);
-          if (chunk + 2 < n_chunks) load_chunk(chunk + 2);
-          load_scales(chunk + 1);
-          asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        } else {
+    } else {
+      f32x16 S0 = f32x16{};                    // scores of the chunk's first block
+      if (working) {
+        u32x4 kr[4];
+        read_k<0>(k_off, kr);
+        S0 = scores(kr);
+      }
+      // A chunk: its two blocks, each with the next block's score products in front of its own exponentials.  Between the
+      // blocks the next chunk is made sure of and the one after it requested, for the buffer that every wave has read to
+      // its end by then.
+      auto one = [&](int chunk, auto which) -> bool {
+        constexpr int p = decltype(which)::value, AT = p * kBuf, NEXT = (p + 1) % 3 * kBuf;
+        const int key0 = chunk * kBlock;
+        const bool more = chunk + 1 < n_chunks, second = key0 + 32 < n_keys;
+        f32x16 S1;
+        asm volatile("" : "=v"(S1));           // (not set where there is no second block, and not used then)
+        if (working) {
+          u32x2 va[8];
+          if (second) {
+            u32x4 kr[4];
+            read_k<AT + 32 * kRow>(k_off, kr);
+            S1 = scores(kr);
+          }
+          read_v<AT + kBlock * kRow>(v_off, va);
+          __builtin_amdgcn_sched_barrier(0);
+          mask(S0, key0);
+          absorb(S0, va, 1.f, 0.f, 1.f);
+        }
+        if (more) {
           wait_vmcnt<0>();
           asm volatile("s_barrier" ::: "memory");
           if (chunk + 2 < n_chunks) issue_chunk(chunk + 2, (p + 2) % 3);
         }
-      }
-      if (working && second) {
-        u32x2 va[8];
-        if (more) {
-          u32x4 kr[4];
-          read_k<NEXT>(k_off, kr);
-          S0 = scores(kr);
+        if (working && second) {
+          u32x2 va[8];
+          if (more) {
+            u32x4 kr[4];
+            read_k<NEXT>(k_off, kr);
+            S0 = scores(kr);
+          }
+          read_v<AT + (kBlock + 32) * kRow>(v_off, va);
+          __builtin_amdgcn_sched_barrier(0);
+          mask(S1, key0 + 32);
+          absorb(S1, va, 1.f, 0.f, 1.f);
         }
-        read_v<AT + (kBlock + 32) * kRow>(v_off, va);
-        __builtin_amdgcn_sched_barrier(0);
-        absorb(S1, va, key0 + 32, ks, lv, iv);
+        return more;
+      };
+      for (int chunk = 0;; chunk += 3) {
+        if (!one(chunk, std::integral_constant<int, 0>{})) break;
+        if (!one(chunk + 1, std::integral_constant<int, 1>{})) break;
+        if (!one(chunk + 2, std::integral_constant<int, 2>{})) break;
       }
-      return more;
-    };
-    for (int chunk = 0;; chunk += 3) {
-      if (!one(chunk, std::integral_constant<int, 0>{})) break;
-      if (!one(chunk + 1, std::integral_constant<int, 1>{})) break;
-      if (!one(chunk + 2, std::integral_constant<int, 2>{})) break;
     }
   }
 
@@ -983,11 +1045,12 @@ int parts_of(int64_t tiles, int64_t rows, int64_t kv_len) {
 
 // Whether rows share K and V through LDS (k_cross_tiles, k_cross_tiles_f32): from so many tiles of 32 rows on, and two or
 // more of a pair.  (Tiles, keys), us, shared / each tile its own: bf16 (352, 1024) 17.9 / 16.6, (512, 1024) 18.2 / 24.0, (1024, 1024)
-// 20.1 / 42.3; codes (512, 1024) 22.2 / 20.4, (960, 1024) 28.7 / 32.0, (2048, 1024) 31.8 / 53.9; fp32 (960, 1024) 131 / 97, (1408, 1024) 136 /
+// 20.1 / 42.3; codes (512, 1024) 24.3 / 19.6, (640, 1024) 24.5 / 24.3, (960,
+// 1024) 24.2 / 30.2, (1920, 1024) 31.4 / 50.6; fp32 (960, 1024) 131 / 97, (1408, 1024) 136 /
 // 133, (2048, 1024) 139 / 181.
 template <int KIND> bool shares_rows(const CrossArgs& a) {
   // (64 rows of K or V span less than 4 GiB, see issue_chunk)
-  const int64_t least = KIND == kF32 ? 1800 : KIND == kCodes ? 768 : 448;
+  const int64_t least = KIND == kF32 ? 1800 : KIND == kCodes ? 672 : 448;
   return a.parts == 1 && a.tiles > 1 && a.ks[2] < (1 << 23) && (int64_t)a.B * a.Hkv * a.tiles >= least;
 }
 
@@ -1023,10 +1086,12 @@ template <int KIND> litevar_status launch(CrossArgs& a, float c, hipStream_t st)
   if (shares_rows<KIND>(a)) {
     // Eight waves to a workgroup read K and V half as often; four waste less on few tiles and leave less of the chip idle:
     // (tiles of a pair, pairs), 1024 keys, eight / four: (8, 64) 21.4 / 18.2; (22, 64) 23.0 / 25.2; (8, 256) 25.9 / 27.8; (22, 480) 106 / 118.
-    // On codes eight spill registers, (8, 480) 53.0 / 54.1, (8, 256) 33.8 / 31.8, and of workgroups of six a CU holds one: (6, 480),
-    // 256 keys, six / four 22.9 / 21.0, (8, 480) 39.2 / 22.0.
-    const int nwv = KIND == kBf16 && a.tiles > 4 && (int64_t)a.B * a.Hkv * ((a.tiles + 7) / 8) >= 192 ? 8 : 4;
-    const int64_t pairs = (int64_t)a.B * a.Hkv;
+    // On codes eight also convert them half as often: from more workgroups of four on than there are CUs, unless there are more of
+    // eight than are resident at once and these idle more: (8, 120) 28.1 / 24.2, (8, 130) 28.2 / 29.9, (6, 480) 42.8 / 48.9, (9, 480) 78.4 / 66.8.
+    const int64_t pairs = (int64_t)a.B * a.Hkv, fours = (a.tiles + 3) / 4, eights = (a.tiles + 7) / 8;
+    const bool eight = KIND == kBf16 ? a.tiles > 4 && pairs * eights >= 192
+                                     : KIND == kCodes && pairs * fours > 256 && (pairs * eights <= 512 || fours == 2 * eights);
+    const int nwv = eight ? 8 : 4;
     a.groups = (a.tiles + nwv - 1) / nwv; a.groups_magic = magic_of(a.groups);
     a.by_xcd = 9 * pairs >= 8 * ((pairs + 7) / 8 * 8);         // (288 pairs of 2240 rows: 93.0 us pair by pair in turn, 91.7 so)
     const int64_t blocks = (a.by_xcd ? (pairs + 7) / 8 * 8 : pairs) * a.groups;
@@ -1036,7 +1101,7 @@ template <int KIND> litevar_status launch(CrossArgs& a, float c, hipStream_t st)
       if constexpr (KIND == kF32) {
         hipLaunchKernelGGL(k_cross_tiles_f32, dim3(n), dim3(256), 0, st, a, c);
       }
-      else if (nwv == 8) hipLaunchKernelGGL((k_cross_tiles<8, kBf16>), dim3(n), dim3(512), 0, st, a, c);
+      else if (nwv == 8) hipLaunchKernelGGL((k_cross_tiles<8, KIND>), dim3(n), dim3(512), 0, st, a, c);
       else hipLaunchKernelGGL((k_cross_tiles<4, KIND>), dim3(n), dim3(256), 0, st, a, c);
     });
   }

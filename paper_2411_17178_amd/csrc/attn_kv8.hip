@@ -26,7 +26,7 @@ namespace {
 // Four codes of a word as floats, exactly.
 __device__ inline void unpack4(unsigned w, float (&x)[4]) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] = (float)(int8_t)((w >> (8 * e)) & 0xffu);
+  for (int e = 0; e < 4; ++e) x[e] = (float)((int)(w << (24 - 8 * e)) >> 24);
 }
 __device__ inline bf16x8 codes_to_bf16(unsigned lo, unsigned hi) {
   float a[4], b[4];

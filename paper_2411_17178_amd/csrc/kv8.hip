@@ -164,7 +164,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_kv8_load(LoadArgs a) {
     typedef __attribute__((ext_vector_type(8))) T T8;
     T8 r;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = (T)(s * (float)(int8_t)(((e < 4 ? c[i].x : c[i].y) >> (8 * (e & 3))) & 0xffu));
+    for (int e = 0; e < 8; ++e) r[e] = (T)(s * (float)((int)((e < 4 ? c[i].x : c[i].y) << (24 - 8 * (e & 3))) >> 24));
     if (8 * i + row8 < k.rows) *(T8*)(out + (8 * i + row8) * 64) = r;
   }
 }

@@ -80,6 +80,8 @@ SHAPES = [  # B, H, H_kv, q_len, kv_len
     # rows that share K and V through LDS, in four and in eight waves; with shared heads
     (8, 32, 32, 257, 200), (16, 32, 32, 100, 77), (16, 32, 8, 140, 130), (8, 64, 64, 300, 33), (4, 64, 64, 1000, 1), (16, 32, 32, 130, 0),
     (8, 64, 64, 530, 130), (16, 32, 32, 700, 65), (31, 34, 17, 300, 97),
+    # few pairs of many rows (codes: four waves), on more blocks than a wave holds scales of
+    (2, 24, 24, 500, 330), (1, 24, 24, 1000, 4300), (2, 160, 160, 150, 4165),
 ]
 # (rows of a call that share K and V through LDS, whatever the type: 2560 tiles)
 MANY = (16, 32, 130)
