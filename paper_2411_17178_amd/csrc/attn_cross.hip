@@ -1030,14 +1030,17 @@ namespace {
 // they leave.  That is least at sqrt(1355 blocks / rows) parts; with fewer than three, few blocks, or a tile for nearly every
 // CU there is nothing to gain.  (Tiles, rows, blocks), bf16, us without / with as many parts as given here: (1, 1, 64) 26.2 / 8.7 (64);
 // (8, 256, 64) 27.9 / 10.4 (18); (32, 1024, 64) 31.4 / 13.4 (9); (128, 4096, 64) 36.5 / 25.6 (4); (128, 4096, 256) 124 / 56 (4);
-// declined: (64, 64, 4) 5.8 / 7.9 (4); (256, 256, 64) 40.2 / 46.2 (4); (256, 6400, 64) 39.7 / 41.4 (4).
+// (192, 4992, 165) 80 / 58 (5); (200, 6000, 125) 64 / 50 (5); (260, 5200, 94) 62 / 56 (3); (300, 9600, 125) 91 / 86 (3);
+// declined: (256, 8192, 188) 118 / 100 (4), fp32 257 / 285; (220, 7040, 63) 35.6 / 38.1 (3); (400, 12800, 157) 117 / 155 (2); (64, 64, 4) 5.8 / 7.9 (4); (256, 256, 64) 40.2 / 46.2 (4); (256, 6400, 64) 39.7 / 41.4 (4).
 int parts_of(int64_t tiles, int64_t rows, int64_t kv_len) {
   const int64_t blocks = (kv_len + kBlock - 1) / kBlock;
-  if (tiles < 1 || tiles >= 200 || blocks <= 8) return 1;
+  const bool long_axis = blocks >= 80;
+  if (tiles < 1 || tiles >= (long_axis ? 320 : 200) || (tiles > 224 && tiles <= 256) || blocks <= 8) return 1;
   int64_t most = blocks / 16 < 64 ? 64 : blocks / 16;
   if (most > kMaxParts) most = kMaxParts;
   if (most > blocks) most = blocks;
-  if (most > 512 / tiles) most = 512 / tiles;
+  const int64_t items = long_axis && tiles > 128 ? 1024 : 512;   // (workgroups)
+  if (most > items / tiles) most = items / tiles;
   int64_t p = (int64_t)std::sqrt(1355.0 * (double)blocks / (double)rows);
   if (p > most) p = most;
   return p < 3 ? 1 : (int)p;

@@ -82,6 +82,8 @@ SHAPES = [  # B, H, H_kv, q_len, kv_len
     (8, 64, 64, 530, 130), (16, 32, 32, 700, 65), (31, 34, 17, 300, 97),
     # few pairs of many rows (codes: four waves), on more blocks than a wave holds scales of
     (2, 24, 24, 500, 330), (1, 24, 24, 1000, 4300), (2, 160, 160, 150, 4165),
+    # parts of a long axis, more workgroups than a round
+    (1, 130, 130, 40, 5200), (3, 100, 50, 60, 5121),
 ]
 # (rows of a call that share K and V through LDS, whatever the type: 2560 tiles)
 MANY = (16, 32, 130)
