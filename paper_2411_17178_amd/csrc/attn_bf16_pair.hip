@@ -315,10 +315,11 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
   [[maybe_unused]] auto block_of = [&](int tok) -> int {
     int shift = __builtin_amdgcn_readlane(my_shift, seg);
     while (seg < gd.k) {
-      const bool beyond = tok >= __builtin_amdgcn_readlane(my_off, seg + 1);
-      if (__builtin_amdgcn_ballot_w64(beyond) == 0) break;
-      ++seg;
-      shift = beyond ? __builtin_amdgcn_readlane(my_shift, seg) : shift;
+      const uint64_t beyond = __builtin_amdgcn_ballot_w64(tok >= __builtin_amdgcn_readlane(my_off, seg + 1));
+      if (beyond == 0) break;
+      seg = __builtin_amdgcn_readfirstlane(seg + 1);     // (the same in all lanes, which the compiler does not find out)
+      const int next = __builtin_amdgcn_readlane(my_shift, seg);
+      shift = __builtin_amdgcn_inverse_ballot_w64(beyond) ? next : shift;
     }
     return (tok + shift) >> 6;
   };
@@ -456,12 +457,12 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
   // The loads go out in the order in which their results are needed: tokens (the transfers of the first three chunks
   // wait for them), step descriptors, Q.  The transfers follow (a load issued behind a chunk is held up until the
   // chunk's data is in), and what needs no memory is formed behind them.
+  int tok0 = load_tok(0), tok1 = load_tok(1), tok2 = load_tok(2);
   if constexpr (KV != 0) {
     for (int i = 64 + lane; i < scales.n_seen; i += 64) { head_k.add(scales.k[scale_row + i]); head_v.add(scales.v[scale_row + i]); }
     const int64_t at = scale_row + min(lane, scales.n_seen - 1);
     first_k = scales.k[at]; first_v = scales.v[at];
   }
-  int tok0 = load_tok(0), tok1 = load_tok(1), tok2 = load_tok(2);
   // Step descriptors for one phase: the first step's is fetched during the phase
   // before (d0), those of the next kLater steps at the start of the phase (dl).
   // (Every register that a vector load fills is used only behind an explicit wait for all
@@ -524,8 +525,10 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
   asm volatile("" : "+v"(t0), "+v"(t1), "+v"(t2));      // (all three formed before the first transfer)
   [[maybe_unused]] float scale0 = 0.f;
   if constexpr (KV == 2) {
-    scale0 = scale_of(t0); scale1 = scale_of(t1); scale2 = scale_of(t2);
+    // (the blocks are found while the codes are on their way; all of it is waited for)
     issue_codes(0, t0); issue_codes(1, t1); issue_codes(2, t2);
+    __builtin_amdgcn_sched_barrier(0);
+    scale0 = scale_of(t0); scale1 = scale_of(t1); scale2 = scale_of(t2);
   } else if constexpr (Q8) {
     // through registers: the three chunks are requested together, converted and written, and
     // the first barrier finds all of them in the ring
@@ -559,9 +562,12 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
     asm volatile("" : "+v"(ones));   // kept in four registers (the compiler would rebuild it in every step)
   }
   // everything older than chunks 1 and 2 is in: Q, the descriptors and tokens, chunk 0 (Q8: all three chunks)
-  if constexpr (Q8) wait_vmcnt<0>(); else if constexpr (KV == 2) wait_vmcnt<2>(); else wait_vmcnt<2 * kDmaPerChunk>();
+  if constexpr (CODES) wait_vmcnt<0>(); else wait_vmcnt<2 * kDmaPerChunk>();
+  if constexpr (KV != 0) asm volatile("" : "+v"(first_k), "+v"(first_v));      // (not used ahead of the wait)
+  if constexpr (KV == 2) asm volatile("" : : "v"(warm));          // (its only use, see below: no register is left for it)
   [[maybe_unused]] float c_lane = c;           // KV: softmax scale of this lane's query, its and K's powers of two taken out
   [[maybe_unused]] int q_power = 0;
+  [[maybe_unused]] float q_scale = 1.f;
   if constexpr (KV != 0) {
     // (the largest magnitude of the row: bf16 bits without their sign compare as integers, two to a word)
     typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
@@ -574,7 +580,8 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
         top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w));
       }
     const float mx = __uint_as_float((unsigned)(top.x > top.y ? top.x : top.y) << 16);
-    q_power = power_to_14(fmaxf(mx, other_half(mx)));
+    q_power = min(power_to_14(fmaxf(mx, other_half(mx))), 127);     // (its power is a normal number)
+    q_scale = __uint_as_float((unsigned)(q_power + 127) << 23);
     join_scales();
     if (wide_range) ps.far = queries;
     if constexpr (KV == 2) convert_chunk(0, scale0);
@@ -587,7 +594,7 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const unsigned w = q_raw[t][e >> 1];
-        piece[e] = (_Float16)ldexpf(__uint_as_float(e & 1 ? w & 0xffff0000u : w << 16), q_power);
+        piece[e] = (_Float16)(__uint_as_float(e & 1 ? w & 0xffff0000u : w << 16) * q_scale);
       }
     } else if constexpr (Q8) {
       const unsigned w0 = q_raw[t >> 1][2 * (t & 1)], w1 = q_raw[t >> 1][2 * (t & 1) + 1];
@@ -860,22 +867,32 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
     while (run_phase(ph, std::false_type{})) ++ph;
   }
 
-  asm volatile("" : : "v"(warm));      // the only use of the plan-touching load: keeps it
+  if constexpr (KV != 2) asm volatile("" : : "v"(warm));      // the only use of the plan-touching load: keeps it
 
   // ---- epilogue ----
   int n_again = n;                             // recomputed from scratch: the row is not worth a
   asm volatile("" : "+v"(n_again));            // register (or a spill slot) through the loop
   int qrow = query_row(n_again, false);
   if constexpr (WIDE) {
-    const float sum = ps.L + other_half(ps.L), inv = 1.f / sum;
+    const float sum = ps.L + other_half(ps.L);
+    float inv = 1.f / sum;
+    if constexpr (KV != 0) {
+      // V's power of two, with the division where both together are a normal number (the sum is between 2^-3 and 2^27)
+      if (__builtin_expect(v_power > -90 && v_power < 90, 1)) {
+        inv = ldexpf(inv, -v_power);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) { ps.O[0][e] = ldexpf(ps.O[0][e] * inv, -v_power); ps.O[1][e] = ldexpf(ps.O[1][e] * inv, -v_power); }
+        inv = 1.f;
+      }
+    }
     float any = 0.f;
     unsigned r[2][8];
 #pragma unroll
     for (int dt = 0; dt < 2; ++dt)
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
-        float x = ps.O[dt][e] * inv, y = ps.O[dt][e + 1] * inv;
-        if constexpr (KV != 0) { x = ldexpf(x, -v_power); y = ldexpf(y, -v_power); }
+        const float x = ps.O[dt][e] * inv, y = ps.O[dt][e + 1] * inv;
         const bf16x2 two = {(__bf16)x, (__bf16)y};
         any = __builtin_amdgcn_fdot2_f32_bf16(two, kOnes, any, false);
         r[dt][e / 2] = __builtin_bit_cast(unsigned, two);
