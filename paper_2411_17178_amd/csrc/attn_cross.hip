@@ -10,10 +10,10 @@
 // shares_rows and parts_of choose, by measured cost.
 //
 // What a call cannot do without: Q, O and the valid keys' K and V once, 256 operations per row and key.  256 rows, 480 pairs of 77 to 512
-// keys, bf16: 22.9 us for 73 MB (14.4 at the copy rate); 2240 rows, 32 pairs, fp32: 56 us for 4.2 TFLOP (27 at a large
+// keys, bf16: 22.4 us for 73 MB (14.4 at the copy rate); 2240 rows, 32 pairs, fp32: 56 us for 4.2 TFLOP (27 at a large
 // product's rate); four rows (one token, 4 query
 // heads) on up to 30 011 keys in codes, 16 pairs: 17.7 us for 44 MB (8.7); 169 rows, 480 pairs of 51 to 333
-// keys in codes: 18.1 us (7.0).
+// keys in codes: 17.5 us (7.0).
 #include <cmath>
 #include <cstring>
 #include <type_traits>
@@ -46,6 +46,7 @@ struct CrossArgs {
   uint32_t q_magic, tiles_magic, hkv_magic, parts_magic, pairs_magic;   // see divmod_by
   uint32_t first_block, rows_magic;
   int groups, by_xcd; uint32_t groups_magic;   // k_cross_tiles: workgroups of a pair, how they are laid out
+  uint32_t prio_magic;                         // 2^18 / chunks of the longest axis, 0: no priorities
   float* part_o; float2* part_ml;              // [item][32][64] and [item][32] (largest score, sum), item = workgroup
 };
 
@@ -670,6 +671,17 @@ void k_cross_tiles(CrossArgs a, float c) {
       }
   };
 
+  // A wave's priority falls with the chunks that it still has: the scheduler prefers the oldest workgroup of a CU, and the
+  // one after it would be left to work alone, at half the rate
+  auto set_priority = [&](int chunk) {
+    if (a.prio_magic == 0) return;
+    switch (((uint32_t)(n_chunks - 1 - chunk) * a.prio_magic) >> 16) {
+      case 0: __builtin_amdgcn_s_setprio(0); break;
+      case 1: __builtin_amdgcn_s_setprio(1); break;
+      case 2: __builtin_amdgcn_s_setprio(2); break;
+      default: __builtin_amdgcn_s_setprio(3);
+    }
+  };
   if (n_chunks > 0) {
     if constexpr (CODES) {
       const float ks = a.k_scale[scales_at(0)], vs = a.v_scale[scales_at(0)];
@@ -693,6 +705,7 @@ void k_cross_tiles(CrossArgs a, float c) {
       // A chunk: the score products of both blocks, then their exponentials.  In between the next chunk is converted into
       // the other buffer, which nobody has read since the barrier that let this chunk begin.
       for (int chunk = 0, at = 0;; ++chunk, at = kBuf - at) {
+        set_priority(chunk);
         const float ks = scale_of(lane_ks, chunk), lv = scale_of(lane_lv, chunk), iv = scale_of(lane_iv, chunk);
         const int key0 = chunk * kBlock;
         const bool more = chunk + 1 < n_chunks, second = key0 + 32 < n_keys;
@@ -748,6 +761,7 @@ void k_cross_tiles(CrossArgs a, float c) {
         constexpr int p = decltype(which)::value, AT = p * kBuf, NEXT = (p + 1) % 3 * kBuf;
         const int key0 = chunk * kBlock;
         const bool more = chunk + 1 < n_chunks, second = key0 + 32 < n_keys;
+        set_priority(chunk);
         f32x16 S1;
         asm volatile("" : "=v"(S1));           // (not set where there is no second block, and not used then)
         if (working) {
@@ -1099,6 +1113,10 @@ template <int KIND> litevar_status launch(CrossArgs& a, float c, hipStream_t st)
     a.by_xcd = 9 * pairs >= 8 * ((pairs + 7) / 8 * 8);         // (288 pairs of 2240 rows: 93.0 us pair by pair in turn, 91.7 so)
     const int64_t blocks = (a.by_xcd ? (pairs + 7) / 8 * 8 : pairs) * a.groups;
     if (blocks > 0x7fffffff) return fail(LITEVAR_E_UNSUPPORTED, "grid too large");
+    // Workgroups that share a CU to their end: see set_priority.  (480 pairs of 256 rows on up to 512 keys 25.8 -> 25.0 us, 169 on up to 333
+    // codes 19.6 -> 19.0; with more rounds new workgroups would hold up old ones: 288 pairs of 2240 rows 86.0 -> 90.2.)
+    const int64_t chunks = ((int64_t)a.kv_len + kBlock - 1) / kBlock;
+    a.prio_magic = blocks * nwv <= (KIND == kBf16 && nwv == 4 ? 3072 : 4096) && chunks > 0 ? (uint32_t)((1 << 18) / chunks) : 0;
     return launch_in_parts(blocks, nwv * 64, "cross attention launch", [&](int64_t first, unsigned n) {
       a.first_block = (uint32_t)first;
       if constexpr (KIND == kF32) {
