@@ -216,7 +216,8 @@ struct StepKeys {
 //   KV = 1: K and V are copies in f16 (k_kv8_load), which come by LDS-DMA.
 //   KV = 2: LDS-DMA takes the codes to the ring, where they are converted in place at the end of the phase; no registers
 //     are held in between.  (256 queries on 680 keys, 480 pairs: 39.8 us through registers and with three chunks converted before
-//     the first barrier, as Q8 has it; 34.8 so; 30.2 with K and V in waves of their own.)
+//     the first barrier, as Q8 has it; 34.8 so; 30.2 with K and V in waves of their own; 28.9 with the first codes
+//     requested ahead of the search for their blocks, and a byte converted in one instruction.)
 template <int PW, bool Q8, int KV = 0>
 __global__ __launch_bounds__((kGroupPatches / PW) * 64) __attribute__((amdgpu_waves_per_eu(4, 4)))
 void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV != 0, KV8Scales, NoScales> scales) {

@@ -219,16 +219,16 @@ litevar_status launch_blocks(Blocks& w, const char* what, Launch launch) {
 // How a plan's cache is read.  Plans whose bf16 calls run 32 queries per wave do so here too: with the codes converted in
 // the attention kernel, once per group that streams a row, or from a copy that is converted once; plans of smaller groups,
 // and handles that ask for sixteen waves, gather codes step by step.
-// Rows streamed over rows seen, in the kernel / through a copy, us: 1.04 (480 pairs, 256 queries on 680) 34.0 / 55.9; 1.7 (288,
-// 324 on 650) 44.4 / 49.3; 2.06 (288, 1024 on 2240) 112.9 / 121.9; 3.01 (480, 680) 129.6 / 121.5; (60, 680) 31.9 / 30.7; 3.17 (288,
-// 2240, radius 2) 186.7 / 177.3; 4.06 (288, 2240) 234.9 / 212.6.
+// Rows streamed over rows seen, in the kernel / through a copy, us: 1.04 (480 pairs, 256 queries on 680) 28.9 / 54; 2.06 (288, 1024
+// on 2240) 110.8 / 127.4; 2.74 (288, 2240, radius 1) 140.1 / 163.9; 3.01 (480, 680) 106.6 / 106.9; 3.17 (288, 2240, radius 2) 166.6 / 179.9;
+// 3.57 (radius 3) 187.2 / 197.0; 4.06 (radius 4) 216.6 / 213.5, of 36 pairs 43.3 / 44.2; between 3 and 4 neither is ahead by more than 8 %.
 enum Route { kGather, kInKernel, kCopy };
 Route route_of(const litevar_plan* plan) {
   if (plan->waves_per_group != 16 || plan->patches_per_wave == 1 || (int64_t)plan->kv_len * 128 >= ((int64_t)1 << 31)) return kGather;
   int64_t seen = 0;
   for (int k = 0; k < plan->q_scale_end; ++k) seen += (int64_t)plan->scales[k] * plan->scales[k];
   const int64_t streamed = plan->n_union_keys / (plan->n_head_groups > 0 ? plan->n_head_groups : 1);
-  return 2 * streamed <= 5 * seen ? kInKernel : kCopy;
+  return streamed <= 3 * seen ? kInKernel : kCopy;
 }
 
 // (the stride of an axis with one entry is never used, and is what it is)
