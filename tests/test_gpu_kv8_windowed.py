@@ -212,6 +212,24 @@ def test_distributions_of_scores(lv, route, shift, spread, size):
     plain.assert_close(out, want, _tolerance(A, S, floor))
 
 
+@pytest.mark.parametrize("route", ROUTES, ids=str)
+@pytest.mark.parametrize("k_power,v_power", [(0, -100), (0, 110), (-110, 0), (60, -90), (-60, 89)])
+def test_values_near_the_ends_of_their_type(lv, route, k_power, v_power):
+    """All of K or V very small or very large, queries the other way round: powers of two do not change relative errors."""
+    q_scales, waves = route
+    B, H = 1, 2
+    plan = lv.litevar_mask_build(VAR256, 3, None, 0, q_scales, waves_per_group=waves)
+    cache = lv.litevar_kv8_cache([s * s for s in VAR256], B, H)
+    g = torch.Generator(device="cuda").manual_seed(12)
+    k, v = (torch.randn(B, H, 680, 64, generator=g, device="cuda") for _ in range(2))
+    q = torch.randn(B, H, plan.q_len, 64, generator=g, device="cuda")
+    lv.litevar_kv8_store(cache, k * 2.0 ** k_power, v * 2.0 ** v_power)
+    q = (q * 2.0 ** -k_power).to(torch.bfloat16)
+    out = lv.litevar_windowed_attn_kv8_fwd(plan, q, cache, SM)
+    want, A, S, floor = _reference(cache, q, lv.litevar_mask_export_dense(plan)[0].bool())
+    plain.assert_close(out, want, _tolerance(A, S, floor))
+
+
 @pytest.mark.parametrize("sm", [1e-30, 1e-6, 1.0, 1e4])
 def test_softmax_scales(lv, sm):
     B, H = 1, 2
