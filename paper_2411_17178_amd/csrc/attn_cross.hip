@@ -1116,7 +1116,7 @@ template <int KIND> litevar_status launch(CrossArgs& a, float c, hipStream_t st)
     // Workgroups that share a CU to their end: see set_priority.  (480 pairs of 256 rows on up to 512 keys 25.8 -> 25.0 us, 169 on up to 333
     // codes 19.6 -> 19.0; with more rounds new workgroups would hold up old ones: 288 pairs of 2240 rows 86.0 -> 90.2.)
     const int64_t chunks = ((int64_t)a.kv_len + kBlock - 1) / kBlock;
-    a.prio_magic = blocks * nwv <= (KIND == kBf16 && nwv == 4 ? 3072 : 4096) && chunks > 0 ? (uint32_t)((1 << 18) / chunks) : 0;
+    a.prio_magic = blocks * nwv <= 256 * (KIND == kBf16 && nwv == 4 ? 12 : 16) && chunks > 0 ? (uint32_t)((1 << 18) / chunks) : 0;
     return launch_in_parts(blocks, nwv * 64, "cross attention launch", [&](int64_t first, unsigned n) {
       a.first_block = (uint32_t)first;
       if constexpr (KIND == kF32) {
