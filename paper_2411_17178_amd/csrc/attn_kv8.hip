@@ -83,7 +83,9 @@ __global__ __launch_bounds__(W * 64) void k_attn_kv8(AttnArgs a, KV8Scales ks, i
   for (int j = 0; j < 4; ++j) O[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;          // softmax reference of query n (the same in its four lanes), this lane's row sum
 
-  for (int s = wave; s < n_steps; s += W) {
+  // the rows of a step: scales of key `lane % 32`, codes of the keys above
+  struct Rows { float2 sc; u32x4 kc[2]; unsigned vc[2][4]; };
+  auto load_rows = [&](const Tokens& tok) {
     // (padding keys carry token -1; they read the row of the step's first key, which every step has)
     const int first = __builtin_amdgcn_readfirstlane(tok.own);
     auto row = [&](int t) -> int { return checked_index(a.hdr, t < 0 ? first : t, a.kv_len); };
@@ -91,30 +93,31 @@ __global__ __launch_bounds__(W * 64) void k_attn_kv8(AttnArgs a, KV8Scales ks, i
     int shift = 0;                           // 64 x block = token + shift, rounded down
     for (int j = 1; j <= wd.kq; ++j) shift = own >= ks.off[j] ? ks.shift[j] : shift;
     const int block = (own + shift) >> 6;
-    const float2 sc = make_float2(Ks[block], Vs[block]);
-    u32x4 kc[2];
-    unsigned vc[2][4];
+    Rows r;
+    r.sc = make_float2(Ks[block], Vs[block]);
 #pragma unroll
-    for (int t = 0; t < 2; ++t) kc[t] = *(const u32x4*)(Kp + (int64_t)row(tok.k[t]) * 64 + 16 * g4);
+    for (int t = 0; t < 2; ++t) r.kc[t] = *(const u32x4*)(Kp + (int64_t)row(tok.k[t]) * 64 + 16 * g4);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int vt[4] = {tok.v[t].x, tok.v[t].y, tok.v[t].z, tok.v[t].w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) vc[t][i] = *(const unsigned*)(Vp + (int64_t)row(vt[i]) * 64 + 4 * n);
+      for (int i = 0; i < 4; ++i) r.vc[t][i] = *(const unsigned*)(Vp + (int64_t)row(vt[i]) * 64 + 4 * n);
     }
+    return r;
+  };
+  auto absorb = [&](const Rows& r, int s) {
     const const_u64_ptr mk = (const_u64_ptr)(a.step_mask + (S0 + s) * 8);
     uint64_t keep[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) keep[e] = mk[e];
-    tok = load_tokens(s + W);
-    if (lane < 32) step_scales[wave][lane] = sc;
+    if (lane < 32) step_scales[wave][lane] = r.sc;
     asm volatile("" ::: "memory");           // (read by other lanes of the wave; LDS keeps a wave's order)
 
     f32x4 S[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      S[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16(kc[t][0], kc[t][1]), qv[0], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-      S[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16(kc[t][2], kc[t][3]), qv[1], S[t], 0, 0, 0);
+      S[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16(r.kc[t][0], r.kc[t][1]), qv[0], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+      S[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16(r.kc[t][2], r.kc[t][3]), qv[1], S[t], 0, 0, 0);
     }
     float z[8], vs[8], mx = -INFINITY;
 #pragma unroll
@@ -143,13 +146,29 @@ __global__ __launch_bounds__(W * 64) void k_attn_kv8(AttnArgs a, KV8Scales ks, i
     }
     float v[8][4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) unpack4(vc[e >> 2][e & 3], v[e]);
+    for (int e = 0; e < 8; ++e) unpack4(r.vc[e >> 2][e & 3], v[e]);
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt) {
       bf16x8 vb;
 #pragma unroll
       for (int e = 0; e < 8; ++e) vb[e] = (__bf16)v[e][dt];
       O[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, pb, O[dt], 0, 0, 0);
+    }
+  };
+  // A step's rows are requested ahead of the work on the step before it, their tokens one step earlier (64 queries, 480 pairs, five
+  // steps to a patch 14.7 -> 14.1 us, 64 queries, 120 pairs 7.7 -> 7.1)
+  if (wave < n_steps) {
+    Rows even = load_rows(tok), odd;
+    tok = load_tokens(wave + W);
+    for (int s = wave;; s += 2 * W) {
+      if (s + W >= n_steps) { absorb(even, s); break; }
+      odd = load_rows(tok);
+      tok = load_tokens(s + 2 * W);
+      absorb(even, s);
+      if (s + 2 * W >= n_steps) { absorb(odd, s + W); break; }
+      even = load_rows(tok);
+      tok = load_tokens(s + 3 * W);
+      absorb(odd, s + W);
     }
   }
 
