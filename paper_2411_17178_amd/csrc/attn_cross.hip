@@ -10,7 +10,7 @@
 // shares_rows and parts_of choose, by measured cost.
 //
 // What a call cannot do without: Q, O and the valid keys' K and V once, 256 operations per row and key.  256 rows, 480 pairs of 77 to 512
-// keys, bf16: 22.4 us for 73 MB (14.4 at the copy rate); 2240 rows, 32 pairs, fp32: 56 us for 4.2 TFLOP (27 at a large
+// keys, bf16: 22.4 us for 73 MB (14.4 at the copy rate); 2240 rows, 32 pairs, fp32: 53 us for 4.2 GFLOP (27 at a large
 // product's rate); four rows (one token, 4 query
 // heads) on up to 30 011 keys in codes, 16 pairs: 17.7 us for 44 MB (8.7); 169 rows, 480 pairs of 51 to 333
 // keys in codes: 17.5 us (7.0).
@@ -45,7 +45,7 @@ struct CrossArgs {
   int scale_blocks;                            // of a (batch, kv head)
   uint32_t q_magic, tiles_magic, hkv_magic, parts_magic, pairs_magic;   // see divmod_by
   uint32_t first_block, rows_magic;
-  int groups, by_xcd; uint32_t groups_magic;   // k_cross_tiles: workgroups of a pair, how they are laid out
+  int groups, by_xcd, by_rank; uint32_t groups_magic;   // k_cross_tiles: workgroups of a pair, how they are laid out
   uint32_t prio_magic;                         // 2^18 / chunks of the longest axis, 0: no priorities
   float* part_o; float2* part_ml;              // [item][32][64] and [item][32] (largest score, sum), item = workgroup
 };
@@ -59,6 +59,20 @@ __device__ inline Row row_at(const CrossArgs& a, int j, int r) {
 }
 
 __device__ inline int keys_of(const CrossArgs& a, int b) { return a.len ? min(max(a.len[b], 0), a.kv_len) : a.kv_len; }
+
+// The batch row that is r-th in the order of lengths, longest first, and its number of keys: where workgroups follow others on
+// a CU, those that run longest start first.  (By chunks of 64 keys, ties in the order of rows; every lane of a wave counts the rows
+// ahead of its own.  288 pairs of 2240 rows on 149 to 512 keys: 86.0 -> 78.5 us in a graph.)
+__device__ inline int batch_of_rank(const CrossArgs& a, int r, int& n_keys) {
+  if (!a.by_rank) { n_keys = keys_of(a, r); return r; }
+  const int lane = lane_of_wave(), keys = min(max(a.len[min(lane, a.B - 1)], 0), a.kv_len);
+  const unsigned key = ((unsigned)keys + (kBlock - 1u)) / kBlock * 64u + (63u - (unsigned)lane);
+  int rank = 0;
+  for (int i = 0; i < a.B; ++i) rank += (unsigned)__builtin_amdgcn_readlane((int)key, i) > key;
+  const int b = __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < a.B && rank == r));
+  n_keys = __builtin_amdgcn_readlane(keys, b);
+  return b;
+}
 
 // a value that is the same in all lanes, in a scalar register
 __device__ inline float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
@@ -501,7 +515,9 @@ void k_cross_tiles(CrossArgs a, float c) {
     divmod_by(block, (uint32_t)(a.B * a.Hkv), a.pairs_magic, tile, bj);
   }
   divmod_by((uint32_t)bj, (uint32_t)a.Hkv, a.hkv_magic, b, j);
-  const int n_keys = keys_of(a, b);
+  int n_keys;
+  b = batch_of_rank(a, b, n_keys);
+  bj = b * a.Hkv + j;
   const int row0 = (tile * NWV + wave) * kRows;
   const bool working = row0 < a.rows;          // (uniform)
   bf16x8 qf[4];
@@ -838,7 +854,10 @@ void k_cross_tiles_f32(CrossArgs a, float c) {
     divmod_by(block, (uint32_t)(a.B * a.Hkv), a.pairs_magic, tile, bj);
   }
   divmod_by((uint32_t)bj, (uint32_t)a.Hkv, a.hkv_magic, b, j);
-  const int n_keys = keys_of(a, b), row0 = (tile * NWV + wave) * kRows;
+  int n_keys;
+  b = batch_of_rank(a, b, n_keys);
+  bj = b * a.Hkv + j;
+  const int row0 = (tile * NWV + wave) * kRows;
   const bool working = row0 < a.rows;          // (uniform)
   float qf[32];
   {
@@ -1116,7 +1135,9 @@ template <int KIND> litevar_status launch(CrossArgs& a, float c, hipStream_t st)
     // Workgroups that share a CU to their end: see set_priority.  (480 pairs of 256 rows on up to 512 keys 25.8 -> 25.0 us, 169 on up to 333
     // codes 19.6 -> 19.0; with more rounds new workgroups would hold up old ones: 288 pairs of 2240 rows 86.0 -> 90.2.)
     const int64_t chunks = ((int64_t)a.kv_len + kBlock - 1) / kBlock;
-    a.prio_magic = blocks * nwv <= 256 * (KIND == kBf16 && nwv == 4 ? 12 : 16) && chunks > 0 ? (uint32_t)((1 << 18) / chunks) : 0;
+    const bool resident = blocks * nwv <= 256 * (KIND == kCodes || nwv == 8 ? 16 : KIND == kBf16 ? 12 : 8);
+    a.prio_magic = KIND != kF32 && resident && chunks > 0 ? (uint32_t)((1 << 18) / chunks) : 0;
+    a.by_rank = !resident && a.len && a.B > 1 && a.B <= 64;     // (a lane for each row)
     return launch_in_parts(blocks, nwv * 64, "cross attention launch", [&](int64_t first, unsigned n) {
       a.first_block = (uint32_t)first;
       if constexpr (KIND == kF32) {

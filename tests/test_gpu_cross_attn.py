@@ -82,6 +82,8 @@ SHAPES = [  # B, H, H_kv, q_len, kv_len
     (8, 64, 64, 530, 130), (16, 32, 32, 700, 65), (31, 34, 17, 300, 97),
     # few pairs of many rows (codes: four waves), on more blocks than a wave holds scales of
     (2, 24, 24, 500, 330), (1, 24, 24, 1000, 4300), (2, 160, 160, 150, 4165),
+    # more batch rows than a wave has lanes, and as many
+    (70, 12, 12, 140, 97), (64, 12, 6, 140, 97), (65, 9, 9, 160, 70),
     # parts of a long axis, more workgroups than a round
     (1, 130, 130, 40, 5200), (3, 100, 50, 60, 5121),
 ]
