@@ -209,9 +209,9 @@ struct StepKeys {
 // KV (an 8-bit cache with block scales, bf16 queries): the products run on f16.  A head's K values are multiplied by the
 // power of two that puts its largest block scale near 2^7 (values below 2^14), V's likewise, every query by its own; the
 // powers leave through the softmax scale of the lane and the stored result.  f16 holds three bits more than bf16: a code
-// times its scale is off by 2^-12 at most, a probability by 2^-11 (towards zero, in the sum and the products alike; weights
+// times its scale is off by 2^-11 at most, a probability by 2^-10 (towards zero, in the sum and the products alike; weights
 // below 2^-11 of the row's sum by up to 2^-21 of it, where f16 is subnormal).  With bf16 in their place the result was off by 0.0033
-// relative to its norm, by 0.0017 so, which  Heads whose block scales differ by more than 2^20
+// relative to its norm, by 0.0017 so, most of it the rounding of the stored result.  Heads whose block scales differ by more than 2^20
 // would lose bits of the smaller blocks: all their rows are formed again from the codes.
 //   KV = 1: K and V are copies in f16 (k_kv8_load), which come by LDS-DMA.
 //   KV = 2: LDS-DMA takes the codes to the ring, where they are converted in place at the end of the phase; no registers

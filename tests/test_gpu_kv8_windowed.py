@@ -2,8 +2,9 @@
 
 Tolerance, element by element (A = sum of weights x |v|, S = the row's largest sum of |q_d k_d| x sm_scale, U = half a
 step of bf16): probabilities rounded, or their products with the V scales, 2 U A; output rounded, U A; V rounded to f16,
-2^-12 A; K rounded to f16, which moves a score by 2^-12 S at most and so a weight by the factor exp(2^-11 S):
-(exp(2^-11 S) - 1) 2 A.  Sums in 32 bits: below U A / 8.  Probabilities in f16 have an absolute floor as well: their last bit is 2^-24 below 2^-14, and a row's sum is at least
+2^-11 A = U A / 8; K rounded to f16, which moves a score by 2^-11 S at most and so a weight, the sum included, by the factor
+exp(2^-10 S): (exp(2^-10 S) - 1) A, of which the tests allow 2 (exp(2^-11 S) - 1) A, which is less.  Sums in 32 bits: below U A / 8.
+Probabilities in f16 have an absolute floor as well: their last bit is 2^-24 below 2^-14, and a row's sum is at least
 2^-3 (it starts at a reference of 0, and a step that leaves the sum below 2^-3 is formed again under a reference that
 makes its largest probability at least 2^-0.5), so a weight is off by 2^-21 at most; over n kept keys with |v| <= V the
 result by 2^-21 (n V + n |out|) <= 2^-20 n V."""
