@@ -6,14 +6,15 @@
 // Two forms.  Few rows (k_cross_rows): one workgroup = four waves = 32 rows of one (batch, kv head) and one part of the
 // key axis; the waves take the part's blocks of 64 keys (32 in fp32) in turn and join their results through LDS.  With
 // several parts, each leaves its sums in the workspace and a second launch joins them (k_cross_join).  Many rows
-// (k_cross_tiles, k_cross_tiles_f32): the waves of a workgroup have 32 rows each and share all keys through LDS.
-// shares_rows and parts_of choose, by measured cost.
+// (k_cross_tiles, k_cross_tiles_f32): the waves of a workgroup have 32 rows each and share all keys, or those of a part of
+// a long axis, through LDS.  shares_rows, shared_parts_of and parts_of choose, by measured cost.
 //
 // What a call cannot do without: Q, O and the valid keys' K and V once, 256 operations per row and key.  256 rows, 480 pairs of 77 to 512
 // keys, bf16: 22.4 us for 73 MB (14.4 at the copy rate); 2240 rows, 32 pairs, fp32: 53 us for 4.2 GFLOP (27 at a large
 // product's rate); four rows (one token, 4 query
 // heads) on up to 30 011 keys in codes, 16 pairs: 17.7 us for 44 MB (8.7); 169 rows, 480 pairs of 51 to 333
 // keys in codes: 17.5 us (7.0).
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <type_traits>
@@ -41,7 +42,7 @@ struct CrossArgs {
   const int32_t* len;                          // [B] or nullptr
   int B, H, Hkv, G, q_len, kv_len;
   int rows, tiles;                             // rows of a kv head, tiles of 32 of them
-  int parts;                                   // of the key axis
+  int parts, shared_parts;                     // of the key axis; those of k_cross_tiles
   int scale_blocks;                            // of a (batch, kv head)
   uint32_t q_magic, tiles_magic, hkv_magic, parts_magic, pairs_magic;   // see divmod_by
   uint32_t first_block, rows_magic;
@@ -473,6 +474,30 @@ __device__ inline void store_tile(const CrossArgs& a, float c, int b, int j, int
   }
 }
 
+// What store_tile does for a part of the key axis: products (times unit), reference and sum of a wave's 32 rows for k_cross_join;
+// a reference of +inf asks it to form the row again.
+template <int KIND>
+__device__ inline void keep_part(const CrossArgs& a, int bj, int part, int n_keys, int row0, const f32x16 (&O)[2], float share,
+                                 float negm, float unit, uint64_t far, uint64_t moved) {
+  const int lane = lane_of_wave(), n = lane & 31;
+  const float l = share + other_half(share);
+  const int64_t row = (((int64_t)bj * a.tiles + row0 / kRows) * a.parts + part) * kRows + n;
+  float any = 0.f;
+  float* o = a.part_o + row * 64 + 4 * (lane >> 5);
+#pragma unroll
+  for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {          // dims 32 dt + 2 e + 4 (lane / 32) .. + 3
+      float4 x = make_float4(O[dt][e], O[dt][e + 1], O[dt][e + 2], O[dt][e + 3]);
+      if constexpr (KIND == kCodes) { x.x *= unit; x.y *= unit; x.z *= unit; x.w *= unit; }
+      any += (x.x + x.y) + (x.z + x.w);
+      *(float4*)(o + 32 * dt + 2 * e) = x;
+    }
+  uint64_t bad = far | (__builtin_amdgcn_ballot_w64(not_finite(any)) & (moved | __builtin_amdgcn_ballot_w64(l > (float)n_keys)));
+  bad |= bad >> 32;
+  if (lane < 32) a.part_ml[row] = make_float2(n_keys <= 0 ? -INFINITY : (bad >> n) & 1 ? INFINITY : -negm, l);
+}
+
 // Many rows: NWV waves of one (batch, kv head), each with 32 rows, share the K and V rows, which pass through LDS in chunks
 // of 64 keys, three buffers: one read, one landing, one whose last readers may be behind, so that one barrier per chunk
 // is enough.  All come by LDS-DMA.  The score products of a block of 32 keys are issued ahead of the exponentials of the
@@ -495,7 +520,7 @@ __device__ inline void store_tile(const CrossArgs& a, float c, int b, int j, int
 // 54 instructions and 16 exponentials for 32 rows x 32 keys, about 300 more for a tile's start and end, and Q and O, 34 us
 // at the copy rate, beside which a round of workgroups starts and ends with little else to do.  512 workgroups that stay, each with
 // a run of five or six tiles whose rows of Q come under the tile before: 102 us (the runs are uneven).
-template <int NWV, int KIND>
+template <int NWV, int KIND, bool PARTS>
 __global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(NWV == 4 && KIND == kBf16 ? 3 : 4, NWV == 4 && KIND == kBf16 ? 3 : 4)))
 void k_cross_tiles(CrossArgs a, float c) {
   constexpr bool CODES = KIND == kCodes;
@@ -518,6 +543,14 @@ void k_cross_tiles(CrossArgs a, float c) {
   int n_keys;
   b = batch_of_rank(a, b, n_keys);
   bj = b * a.Hkv + j;
+  // PARTS: the blocks of this part, the first of which counts as block 0 below
+  [[maybe_unused]] int part = 0, first_block = 0;
+  if constexpr (PARTS) {
+    divmod_by((uint32_t)tile, (uint32_t)a.parts, a.parts_magic, tile, part);
+    const int blocks = (n_keys + kBlock - 1) / kBlock;
+    first_block = (int)((int64_t)blocks * part / a.parts);
+    n_keys = min(n_keys, (int)((int64_t)blocks * (part + 1) / a.parts) * kBlock) - first_block * kBlock;
+  }
   const int row0 = (tile * NWV + wave) * kRows;
   const bool working = row0 < a.rows;          // (uniform)
   bf16x8 qf[4];
@@ -531,7 +564,7 @@ void k_cross_tiles(CrossArgs a, float c) {
   __builtin_amdgcn_sched_barrier(0);           // (the loads of Q stay ahead of the transfers, which are counted below)
 
   // ---- loading duty ----
-  const int64_t kv_at = b * a.ks[0] + j * a.ks[1];
+  const int64_t kv_at = b * a.ks[0] + j * a.ks[1] + (int64_t)first_block * kBlock * a.ks[2];
   const int lrow = lane >> 3;
   const unsigned piece_off = (((unsigned)lane & 7u) ^ dense_swizzle((unsigned)lrow)) << 4;
   [[maybe_unused]] const unsigned row_bytes = (unsigned)a.ks[2] * 2u;
@@ -580,7 +613,7 @@ void k_cross_tiles(CrossArgs a, float c) {
   [[maybe_unused]] auto scales_at = [&](int chunk) {
     int lane = lane_of_wave();
     asm volatile("" : "+v"(lane));             // (formed anew: not worth a register through the loop)
-    return (int64_t)bj * a.scale_blocks + min(chunk + lane, n_chunks - 1);
+    return (int64_t)bj * a.scale_blocks + first_block + min(chunk + lane, n_chunks - 1);
   };
   [[maybe_unused]] auto set_scales = [&](float ks, float vs) {
     lane_ks = ks;
@@ -819,7 +852,9 @@ void k_cross_tiles(CrossArgs a, float c) {
     }
   }
 
-  if (working) store_tile<KIND>(a, c, b, j, bj, n_keys, row0, O, L[0] + L[1], CODES ? vmax : 1.f, far, moved);
+  if (!working) return;
+  if constexpr (PARTS) keep_part<KIND>(a, bj, part, n_keys, row0, O, L[0] + L[1], negm, CODES ? vmax : 1.f, far, moved);
+  else store_tile<KIND>(a, c, b, j, bj, n_keys, row0, O, L[0] + L[1], CODES ? vmax : 1.f, far, moved);
 }
 
 // a lane's half of a K row of 256 bytes, eight pieces; issued only, a wait must precede the first use
@@ -999,9 +1034,9 @@ void k_cross_tiles_f32(CrossArgs a, float c) {
   for (; __builtin_expect(bad != 0, 0); bad &= bad - 1) row_again<kF32>(a, c, b, j, bj, n_keys, row0 + __builtin_ctzll(bad));
 }
 
-// Joins the parts of a row: a workgroup per row, thread t dims 4 (t % 16) .. + 3 of the parts t / 16, + 16, ...
+// Joins the parts of a row (references times unit are in base 2): a workgroup per row, thread t dims 4 (t % 16) .. + 3 of the parts t / 16, + 16, ...
 template <int KIND>
-__global__ __launch_bounds__(256) void k_cross_join(CrossArgs a, float c) {
+__global__ __launch_bounds__(256) void k_cross_join(CrossArgs a, float unit, float c) {
   __shared__ float weight[kMaxParts], wave_m[4], wave_l[4];
   __shared__ __align__(16) float4 sums[16][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -1023,11 +1058,15 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossArgs a, float c) {
   if (lane == 0) wave_m[wave] = m;
   __syncthreads();
   m = fmaxf(fmaxf(wave_m[0], wave_m[1]), fmaxf(wave_m[2], wave_m[3]));
+  if (m == INFINITY) {                         // (see keep_part)
+    if (wave == 0) row_again<KIND>(a, c, b, j, bj, keys_of(a, b), r);
+    return;
+  }
   float l = 0.f;
 #pragma unroll
   for (int i = 0; i < kMaxParts / 256; ++i) {
     // (a part without keys: its products were not written, and do not count)
-    const float f = own_m[i] > -INFINITY ? __builtin_amdgcn_exp2f((own_m[i] - m) * c) : 0.f;
+    const float f = own_m[i] > -INFINITY ? __builtin_amdgcn_exp2f((own_m[i] - m) * unit) : 0.f;
     l = fmaf(own_l[i], f, l);
     weight[tid + 256 * i] = own_m[i] > -INFINITY ? f : -1.f;
   }
@@ -1079,6 +1118,17 @@ int parts_of(int64_t tiles, int64_t rows, int64_t kv_len) {
   return p < 3 ? 1 : (int)p;
 }
 
+// Parts of a long key axis where rows share K and V through LDS in 16 and 8 bits: four workgroups of four waves to a CU, eight
+// blocks to a part at least.  (Pairs, tiles of one, blocks), us, bf16 / codes, each tile its own, shared, and in parts: (3, 222, 192) 166 /
+// 190, 181 / 249, 99 / 110; (12, 27, 314) 180 / 195, 294 / 401, 85 / 88; (10, 33, 101) 63 / 70, 97 / 131, 46 / 46; (16, 16, 125) 62 / 57, 119 / 160,
+// 41 / 44; declined: (60, 8, 63) 45 / 49, 62 / 83, 46 / 48; (140, 5, 47) 49 / 54, 58 / 77, 54 / 61.
+int shared_parts_of(int64_t pairs, int64_t tiles, int64_t kv_len) {
+  const int64_t blocks = (kv_len + kBlock - 1) / kBlock, fours = pairs * ((tiles + 3) / 4);
+  if (tiles < 4 || pairs * tiles < 200 || blocks < 80 || fours > 256) return 1;
+  const int64_t p = std::min(1024 / fours, blocks / 8);
+  return (int)std::min(p, (int64_t)kMaxParts);
+}
+
 // Whether rows share K and V through LDS (k_cross_tiles, k_cross_tiles_f32): from so many tiles of 32 rows on, and two or
 // more of a pair.  (Tiles, keys), us, shared / each tile its own: bf16 (352, 1024) 17.9 / 16.6, (512, 1024) 18.2 / 24.0, (1024, 1024)
 // 20.1 / 42.3; codes (512, 1024) 24.3 / 19.6, (640, 1024) 24.5 / 24.3, (960,
@@ -1086,8 +1136,8 @@ int parts_of(int64_t tiles, int64_t rows, int64_t kv_len) {
 // 133, (2048, 1024) 139 / 181.
 template <int KIND> bool shares_rows(const CrossArgs& a) {
   // (64 rows of K or V span less than 4 GiB, see issue_chunk)
-  const int64_t least = KIND == kF32 ? 1800 : KIND == kCodes ? 672 : 448;
-  return a.parts == 1 && a.tiles > 1 && a.ks[2] < (1 << 23) && (int64_t)a.B * a.Hkv * a.tiles >= least;
+  const int64_t least = KIND == kF32 ? 1800 : a.shared_parts > 1 ? 0 : KIND == kCodes ? 672 : 448;
+  return (a.parts == 1 || (KIND != kF32 && a.shared_parts > 1)) && a.tiles > 1 && a.ks[2] < (1 << 23) && (int64_t)a.B * a.Hkv * a.tiles >= least;
 }
 
 uint32_t magic_of(int64_t n) { return (uint32_t)(((uint64_t)1 << 32) / (uint64_t)(n > 1 ? n : 1) - (n <= 1)); }
@@ -1119,43 +1169,53 @@ litevar_status strides_of(const int64_t* s, int B, int heads, int64_t n, int D, 
 
 template <int KIND> litevar_status launch(CrossArgs& a, float c, hipStream_t st) {
   const int64_t tiles = (int64_t)a.B * a.Hkv * a.tiles;
+  auto join_parts = [&](float unit) {
+    return launch_in_parts((int64_t)a.B * a.Hkv * a.rows, 256, "cross attention join launch", [&](int64_t first, unsigned n) {
+      a.first_block = (uint32_t)first;
+      hipLaunchKernelGGL(k_cross_join<KIND>, dim3(n), dim3(256), 0, st, a, unit, c);
+    });
+  };
   if (shares_rows<KIND>(a)) {
     // Eight waves to a workgroup read K and V half as often; four waste less on few tiles and leave less of the chip idle:
     // (tiles of a pair, pairs), 1024 keys, eight / four: (8, 64) 21.4 / 18.2; (22, 64) 23.0 / 25.2; (8, 256) 25.9 / 27.8; (22, 480) 106 / 118.
     // On codes eight also convert them half as often: from more workgroups of four on than there are CUs, unless there are more of
     // eight than are resident at once and these idle more: (8, 120) 28.1 / 24.2, (8, 130) 28.2 / 29.9, (6, 480) 42.8 / 48.9, (9, 480) 78.4 / 66.8.
     const int64_t pairs = (int64_t)a.B * a.Hkv, fours = (a.tiles + 3) / 4, eights = (a.tiles + 7) / 8;
-    const bool eight = KIND == kBf16 ? a.tiles > 4 && pairs * eights >= 192
+    const bool eight = KIND != kF32 && a.shared_parts > 1 ? fours == 2 * eights
+                     : KIND == kBf16 ? a.tiles > 4 && pairs * eights >= 192
                                      : KIND == kCodes && pairs * fours > 256 && (pairs * eights <= 512 || fours == 2 * eights);
     const int nwv = eight ? 8 : 4;
-    a.groups = (a.tiles + nwv - 1) / nwv; a.groups_magic = magic_of(a.groups);
+    a.parts = KIND == kF32 ? 1 : a.shared_parts; a.parts_magic = magic_of(a.parts);
+    a.part_ml = (float2*)((char*)a.part_o + (size_t)tiles * a.parts * kRows * 64 * 4);
+    a.groups = (a.tiles + nwv - 1) / nwv * a.parts; a.groups_magic = magic_of(a.groups);
     a.by_xcd = 9 * pairs >= 8 * ((pairs + 7) / 8 * 8);         // (288 pairs of 2240 rows: 93.0 us pair by pair in turn, 91.7 so)
     const int64_t blocks = (a.by_xcd ? (pairs + 7) / 8 * 8 : pairs) * a.groups;
     if (blocks > 0x7fffffff) return fail(LITEVAR_E_UNSUPPORTED, "grid too large");
     // Workgroups that share a CU to their end: see set_priority.  (480 pairs of 256 rows on up to 512 keys 25.8 -> 25.0 us, 169 on up to 333
     // codes 19.6 -> 19.0; with more rounds new workgroups would hold up old ones: 288 pairs of 2240 rows 86.0 -> 90.2.)
-    const int64_t chunks = ((int64_t)a.kv_len + kBlock - 1) / kBlock;
+    const int64_t chunks = (((int64_t)a.kv_len + kBlock - 1) / kBlock + a.parts - 1) / a.parts;
     const bool resident = blocks * nwv <= 256 * (KIND == kCodes || nwv == 8 ? 16 : KIND == kBf16 ? 12 : 8);
     a.prio_magic = KIND != kF32 && resident && chunks > 0 ? (uint32_t)((1 << 18) / chunks) : 0;
     a.by_rank = !resident && a.len && a.B > 1 && a.B <= 64;     // (a lane for each row)
-    return launch_in_parts(blocks, nwv * 64, "cross attention launch", [&](int64_t first, unsigned n) {
+    litevar_status s = launch_in_parts(blocks, nwv * 64, "cross attention launch", [&](int64_t first, unsigned n) {
       a.first_block = (uint32_t)first;
       if constexpr (KIND == kF32) {
         hipLaunchKernelGGL(k_cross_tiles_f32, dim3(n), dim3(256), 0, st, a, c);
       }
-      else if (nwv == 8) hipLaunchKernelGGL((k_cross_tiles<8, KIND>), dim3(n), dim3(512), 0, st, a, c);
-      else hipLaunchKernelGGL((k_cross_tiles<4, KIND>), dim3(n), dim3(256), 0, st, a, c);
+      else if (a.parts > 1) {
+        if (nwv == 8) hipLaunchKernelGGL((k_cross_tiles<8, KIND, true>), dim3(n), dim3(512), 0, st, a, c);
+        else hipLaunchKernelGGL((k_cross_tiles<4, KIND, true>), dim3(n), dim3(256), 0, st, a, c);
+      }
+      else if (nwv == 8) hipLaunchKernelGGL((k_cross_tiles<8, KIND, false>), dim3(n), dim3(512), 0, st, a, c);
+      else hipLaunchKernelGGL((k_cross_tiles<4, KIND, false>), dim3(n), dim3(256), 0, st, a, c);
     });
+    return s || a.parts == 1 ? s : join_parts(1.f);
   }
   if (litevar_status s = launch_in_parts(tiles * a.parts, kWaves * 64, "cross attention launch", [&](int64_t first, unsigned n) {
         a.first_block = (uint32_t)first;
         hipLaunchKernelGGL(k_cross_rows<KIND>, dim3(n), dim3(kWaves * 64), 0, st, a, c);
       })) return s;
-  if (a.parts == 1) return LITEVAR_OK;
-  return launch_in_parts((int64_t)a.B * a.Hkv * a.rows, 256, "cross attention join launch", [&](int64_t first, unsigned n) {
-    a.first_block = (uint32_t)first;
-    hipLaunchKernelGGL(k_cross_join<KIND>, dim3(n), dim3(256), 0, st, a, c);
-  });
+  return a.parts == 1 ? LITEVAR_OK : join_parts(c);
 }
 
 // What both entry points check and fill; `kind` as in Kind.
@@ -1186,6 +1246,7 @@ litevar_status cross_attention(CrossArgs& a, Kind kind, int32_t B, int32_t H, in
   a.rows = a.G * q_len; a.tiles = (a.rows + kRows - 1) / kRows;
   const int64_t tiles = tiles_of(B, H, H_kv, q_len);
   a.parts = parts_of(tiles, (int64_t)B * H * q_len, kv_len);
+  a.shared_parts = shared_parts_of((int64_t)B * H_kv, a.tiles, kv_len);
   a.scale_blocks = (kv_len + kBlock - 1) / kBlock;
   a.q_magic = magic_of(q_len); a.tiles_magic = magic_of(a.tiles); a.hkv_magic = magic_of(H_kv); a.parts_magic = magic_of(a.parts);
   a.pairs_magic = magic_of((int64_t)B * H_kv); a.rows_magic = magic_of(a.rows);
@@ -1209,7 +1270,8 @@ litevar_status litevar_cross_attn_workspace_bytes(int32_t B, int32_t H, int32_t 
                                                   size_t* out_bytes) {
   if (!out_bytes) return fail(LITEVAR_E_INVALID_ARG, "out_bytes is NULL");
   if (litevar_status s = check_shape(B, H, H_kv, q_len, kv_len)) return s;
-  const int64_t tiles = tiles_of(B, H, H_kv, q_len), parts = parts_of(tiles, (int64_t)B * H * q_len, kv_len);
+  const int64_t pairs = (int64_t)B * H_kv, tiles = tiles_of(B, H, H_kv, q_len);
+  const int64_t parts = std::max(parts_of(tiles, (int64_t)B * H * q_len, kv_len), shared_parts_of(pairs, tiles / pairs, kv_len));
   *out_bytes = parts > 1 ? (size_t)tiles * parts * kRows * (64 * 4 + 8) : 0;
   return LITEVAR_OK;
 }

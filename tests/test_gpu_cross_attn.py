@@ -84,6 +84,8 @@ SHAPES = [  # B, H, H_kv, q_len, kv_len
     (2, 24, 24, 500, 330), (1, 24, 24, 1000, 4300), (2, 160, 160, 150, 4165),
     # more batch rows than a wave has lanes, and as many
     (70, 12, 12, 140, 97), (64, 12, 6, 140, 97), (65, 9, 9, 160, 70),
+    # rows that share K and V, in parts of a long axis: in eight waves and in four, with parts that hold nothing
+    (2, 32, 1, 100, 5200), (16, 16, 1, 32, 5130), (5, 40, 1, 33, 5121), (3, 23, 1, 308, 6000),
     # parts of a long axis, more workgroups than a round
     (1, 130, 130, 40, 5200), (3, 100, 50, 60, 5121),
 ]
@@ -157,6 +159,27 @@ def test_peaked_and_far_scores(lv, kind, B, H, n):
         kk = k.flip(2) if flip else k
         q16, k16 = q.to(torch.bfloat16).float(), kk.to(torch.bfloat16).float()    # (the operands of all kinds)
         out, want, tol = _run(lv, kind, q16, k16, v.to(torch.bfloat16).float(), None)
+        plain.assert_close(out, want, tol)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "codes"])
+@pytest.mark.parametrize("flip", [False, True])
+def test_parts_join_scores_of_all_sizes(lv, kind, flip):
+    """Scores that rise along the axis, from part to part and inside one; the last heads' beyond 2^24, whose rows are formed again."""
+    B, H, n, L = 2, 32, 100, 5200
+    q, k, v = _randn((B, H, n, 64), 31, scale=3.0), _randn((B, 1, L, 64), 32, scale=3.0), _randn((B, 1, L, 64), 33)
+    k = k * torch.linspace(0.01, 2.0, L, device="cuda")[:, None]
+    if flip:
+        k = k.flip(2)
+    q[:, 30:] = 0
+    q[:, 30:, :, 0] = 2.0 ** 24                                              # (a score is then one product)
+    k[..., 0] = torch.linspace(1.0, 127.0, L, device="cuda").round() * 64
+    q, k, v = (x.to(torch.bfloat16).float() for x in (q, k, v))
+    lens = torch.tensor([L, 1300], dtype=torch.int32).cuda()
+    out, want, tol = _run(lv, kind, q[:, :30], k, v, lens)
+    plain.assert_close(out, want, tol)
+    if kind == "bf16":                                                       # (codes of a block differ from these keys)
+        out, want, tol = _run(lv, kind, q, k, v, lens)
         plain.assert_close(out, want, tol)
 
 
