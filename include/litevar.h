@@ -404,8 +404,8 @@ litevar_status litevar_windowed_attn_qkv8_fwd(const litevar_plan* plan, const in
  *     d_k, d_v     DEVICE [B, H, n, 64], n = the tokens of these segments; bf16 or fp32; finite
  *     kv_strides   HOST, element strides of the (B, H, token) axes, multiples of 8; NULL = packed
  *     d_len        optional DEVICE int32 [B]: tokens of the row's sequence, counted from the cache's first token, that
- *                  count.  Rows from there on are not read, do not enter a scale and leave the cache as it was (they
- *                  may hold anything).
+ *                  count (taken as at least 0).  Rows from there on are not read, do not enter a scale and leave the cache
+ *                  as it was (they may hold anything).
  * litevar_kv8_load    d_k_bf16, d_v_bf16 DEVICE bf16 [B, H, L, 64]: the rows of the segments [segment_begin,
  *                     segment_end) as bf16(s * code); other rows are not written.
  * litevar_windowed_attn_kv8_fwd

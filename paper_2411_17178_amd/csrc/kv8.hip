@@ -82,7 +82,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_kv8_store(StoreArgs a) {
   if (!my_block(a.w, tensor, k)) return;
   const int lane = threadIdx.x & 63, row8 = lane >> 3, part = lane & 7;
   int rows = k.rows;
-  if (a.valid) rows = min(rows, a.valid[k.b] - k.token);
+  if (a.valid) rows = min(rows, max(a.valid[k.b], 0) - k.token);   // (a difference that 32 bits hold)
   if (rows <= 0) return;                       // (rows behind the last valid one keep what they hold)
   const T* x = (const T*)(tensor ? a.x[1] : a.x[0]) + k.b * a.xs[0] + k.h * a.xs[1] + (k.token - a.w.off[0]) * a.xs[2] + 8 * part;
   float v[8][8];
