@@ -78,6 +78,11 @@ __device__ inline int batch_of_rank(const CrossArgs& a, int r, int& n_keys) {
 // a value that is the same in all lanes, in a scalar register
 __device__ inline float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
 
+// log2 of a value >= 0 whatever its size (the instruction takes a subnormal value for 0)
+__device__ inline float log2_of(float x) {
+  return x < 0x1p-126f ? __builtin_amdgcn_logf(x * 0x1p24f) - 24.f : __builtin_amdgcn_logf(x);
+}
+
 // eight codes (a word pair) as bf16, exactly
 __device__ inline bf16x8 codes_to_bf16(unsigned lo, unsigned hi) {
   bf16x8 r;
@@ -618,7 +623,7 @@ void k_cross_tiles(CrossArgs a, float c) {
   [[maybe_unused]] auto set_scales = [&](float ks, float vs) {
     lane_ks = ks;
     // (a scale of zero belongs to a block of zeros: any will do)
-    lane_lv = vs > 0.f ? fmaxf(__builtin_amdgcn_logf(vs) - log_vmax, -96.f) : 0.f;
+    lane_lv = vs > 0.f ? fmaxf(log2_of(vs) - log_vmax, -96.f) : 0.f;
     lane_iv = __builtin_amdgcn_exp2f(-lane_lv);
     asm volatile("" : "+v"(lane_ks));          // (its load is waited for here, not wherever the chunks go on)
   };
@@ -738,7 +743,7 @@ void k_cross_tiles(CrossArgs a, float c) {
       vmax = vs;
       for (int at = 64; at < n_chunks; at += 64) vmax = fmaxf(vmax, a.v_scale[scales_at(at)]);
       vmax = wave_max(vmax);
-      log_vmax = uniform(__builtin_amdgcn_logf(vmax));
+      log_vmax = uniform(log2_of(vmax));
       set_scales(ks, vs);
       commit_codes(0);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");

@@ -1,0 +1,60 @@
+"""Cross attention at the ends of its operands' ranges, in every kernel that a call may take.
+
+Tolerance as for the ordinary operands (A = sum of weights x |v|, U = half a step of bf16): probabilities rounded to
+bf16 while the sum is of the rounded ones 2 U A, the output U A, sums in 32 bits below U A / 8."""
+import pytest
+import torch
+
+import _kv8_plain as plain
+
+pytestmark = pytest.mark.gpu
+SM = 0.125
+
+
+@pytest.fixture(scope="module")
+def lv():
+    import paper_2411_17178_amd as m
+    m.load_library()
+    return m
+
+
+def _randn(shape, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(shape, generator=g, device="cuda")
+
+
+# batch, heads, kv heads, rows, keys: rows of their own; in parts of the axis; rows that share K and V through LDS in
+# workgroups of four waves and of eight; shared in parts of a long axis, of eight and of four
+SHAPES = [(1, 6, 6, 40, 320), (2, 4, 4, 3, 5000), (16, 32, 32, 130, 300), (16, 32, 32, 520, 200), (3, 23, 1, 308, 6000), (2, 30, 1, 120, 5200)]
+
+
+def _cross(lv, kind, q, k, v, sm, lens=None):
+    """(output, reference, tolerance); "codes": k and v are stored first."""
+    B, L = q.shape[0], k.shape[2]
+    if kind == "codes":
+        cache = lv.litevar_kv8_store(lv.litevar_kv8_cache([L], B, k.shape[1]), k, v)
+        q = q.to(torch.bfloat16)
+        out = lv.litevar_cross_attn_kv8_fwd(q, cache, sm, lens=lens)
+        k, v = (plain.dequantise(c, s, [L]) for c, s in ((cache.k8, cache.k_scale), (cache.v8, cache.v_scale)))
+    else:
+        q, k, v = (x.to(torch.bfloat16) for x in (q, k, v))
+        out = lv.litevar_cross_attn_fwd(q, k, v, sm, lens=lens)
+    keep = torch.ones(1, 1, 1, L, dtype=torch.bool, device="cuda")
+    if lens is not None:
+        keep = (torch.arange(L, device="cuda")[None] < lens[:, None])[:, None, None]
+    want, A, _ = plain.attention(q, k, v, keep, sm)
+    return out, want, 3.125 * plain.U * A
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("few", [False, True])
+def test_v_scales_that_are_subnormal(lv, shape, few):
+    """V around 2^-120.5, which bf16 holds as normal numbers, with block scales below 2^-126; all blocks, or all but one
+    whose scale is the smallest that is normal."""
+    B, H, Hkv, n, L = shape
+    q, k = _randn((B, H, n, 64), 1), _randn((B, Hkv, L, 64), 2)
+    v = (1 + 0.2 * _randn((B, Hkv, L, 64), 3)) * 2.0 ** -120.5
+    if few:
+        v[:, :, 64:128] *= 4
+    out, want, tol = _cross(lv, "codes", q, k, v, SM)
+    plain.assert_close(out, want, tol)
