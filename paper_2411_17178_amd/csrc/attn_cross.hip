@@ -44,6 +44,7 @@ struct CrossArgs {
   int rows, tiles;                             // rows of a kv head, tiles of 32 of them
   int parts, shared_parts;                     // of the key axis; those of k_cross_tiles
   int scale_blocks;                            // of a (batch, kv head)
+  float ks_least, ks_most;                     // K scales outside multiply the scores, not the softmax scale: see k_cross_tiles
   uint32_t q_magic, tiles_magic, hkv_magic, parts_magic, pairs_magic;   // see divmod_by
   uint32_t first_block, rows_magic;
   int groups, by_xcd, by_rank; uint32_t groups_magic;   // k_cross_tiles: workgroups of a pair, how they are laid out
@@ -667,7 +668,7 @@ void k_cross_tiles(CrossArgs a, float c) {
   };
   // the rest of a block, its V rows requested; ks, lv, iv: of its chunk
   auto absorb = [&](f32x16& S, u32x2 (&va)[8], float ks, float lv, float iv) {
-    if (CODES && ks < 0x1p-100f) {             // (a block of zeros or nearly so: scaled here, c ks would lose its bits)
+    if (CODES && (ks < a.ks_least || ks > a.ks_most)) {   // (scaled here: c ks would lose its bits, a block of zeros, or overflow)
 #pragma unroll
       for (int e = 0; e < 16; ++e) S[e] = S[e] > -INFINITY ? S[e] * ks : S[e];
       ks = 1.f;
@@ -1258,6 +1259,7 @@ litevar_status cross_attention(CrossArgs& a, Kind kind, int32_t B, int32_t H, in
   a.part_o = (float*)d_workspace;
   a.part_ml = (float2*)((char*)d_workspace + (size_t)tiles * a.parts * kRows * 64 * 4);
   const float c = sm_scale * 1.4426950408889634f;
+  a.ks_least = std::max(0x1p-100f, 0x1p-120f / c); a.ks_most = 0x1p120f / c;   // (infinite for the smallest softmax scales)
   hipStream_t st = (hipStream_t)stream;
   if (kind == kF32) return launch<kF32>(a, c, st);
   if (kind == kCodes) return launch<kCodes>(a, c, st);

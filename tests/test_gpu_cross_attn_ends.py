@@ -58,3 +58,21 @@ def test_v_scales_that_are_subnormal(lv, shape, few):
         v[:, :, 64:128] *= 4
     out, want, tol = _cross(lv, "codes", q, k, v, SM)
     plain.assert_close(out, want, tol)
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_softmax_scale_times_block_scale_leaves_the_range(lv, shape):
+    """The product of the two scales is zero or infinite in fp32 though every score is a number: the weights are equal
+    where it is zero or the queries are, and the largest score takes all where it is infinite."""
+    B, H, Hkv, n, L = shape
+    L -= 7                                                                   # (the last block has keys that do not exist)
+    q, k, v = _randn((B, H, n, 64), 4), _randn((B, Hkv, L, 64), 5), _randn((B, Hkv, L, 64), 6)
+    out, want, tol = _cross(lv, "codes", q, k * 2.0 ** -60, v, 1e-30)
+    plain.assert_close(out, want, tol)
+    # scores of one product: 2^-80 x code x scale x 1e3, thousands apart; q of zero in every second row
+    q = torch.zeros_like(q)
+    q[:, :, 1::2, 3] = 2.0 ** -80
+    k = k * 1e37
+    k[:, :, 5, 3], k[:, :, 5, 0] = 6e37, 6e37                                # (the largest: alone in its row)
+    out, want, tol = _cross(lv, "codes", q, k, v, 1e3)
+    plain.assert_close(out, want, tol)
