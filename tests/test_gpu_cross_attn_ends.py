@@ -76,3 +76,65 @@ def test_softmax_scale_times_block_scale_leaves_the_range(lv, shape):
     k[:, :, 5, 3], k[:, :, 5, 0] = 6e37, 6e37                                # (the largest: alone in its row)
     out, want, tol = _cross(lv, "codes", q, k, v, 1e3)
     plain.assert_close(out, want, tol)
+
+
+# 113 tiles of 32 rows in each of two pairs, 82 blocks: the shape that shares K and V in parts in 16 and 8 bits alike
+PARTS = (2, 30, 1, 120, 5200)
+
+
+def _takes_shared_parts(lv, shape):
+    B, H, Hkv, n, L = shape
+    tiles = B * Hkv * -(-(H // Hkv * n) // 32)
+    assert tiles == 226 and lv.litevar_cross_attn_workspace_bytes(*shape) == tiles * 10 * 32 * (64 * 4 + 8)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "codes"])
+@pytest.mark.parametrize("flip", [False, True])
+def test_shared_parts_join_scores_of_all_sizes(lv, kind, flip):
+    """Scores that rise or fall along the axis by more than a part's sums may grow; one batch row is short."""
+    _takes_shared_parts(lv, PARTS)
+    B, H, Hkv, n, L = PARTS
+    q, k, v = 3 * _randn((B, H, n, 64), 10), 3 * _randn((B, Hkv, L, 64), 11), 3 * _randn((B, Hkv, L, 64), 12)
+    k = k * torch.linspace(0.01, 2.0, L, device="cuda")[:, None]
+    k = k.flip(2) if flip else k
+    lens = torch.tensor([L, 1300], dtype=torch.int32).cuda()
+    out, want, tol = _cross(lv, kind, q.to(torch.bfloat16), k, v, SM, lens)
+    plain.assert_close(out, want, tol)
+
+
+def test_shared_parts_on_codes_with_v_scales_far_apart(lv):
+    """V blocks between 2^-90 and 2^60 of one another, from part to part and inside one, and of zeros; K blocks of zeros."""
+    _takes_shared_parts(lv, PARTS)
+    B, H, Hkv, n, L = PARTS
+    q, k, v = _randn((B, H, n, 64), 13), _randn((B, Hkv, L, 64), 14), _randn((B, Hkv, L, 64), 15)
+    for power in (0, 60):
+        v[0, 0, 64 * 8:64 * 16] *= 2.0 ** -90                                # (a part and more)
+        v[0, 0, 64 * 20:64 * 21] *= 2.0 ** power
+        v[0, 0, 64 * 30:64 * 50] = 0
+        v[1, 0, 64::128] *= 2.0 ** -40
+        v[1, 0, 64 * 70:64 * 71] = 0
+        k[1, 0, 64 * 40:64 * 60] = 0
+        out, want, tol = _cross(lv, "codes", q, k, v, SM)
+        plain.assert_close(out, want, tol)
+
+
+@pytest.mark.parametrize("shape", [PARTS, (16, 32, 32, 130, 300), (1, 6, 6, 40, 320)], ids=str)
+@pytest.mark.parametrize("high", [64.0, 2.0 ** 14])
+def test_far_scores_on_codes(lv, shape, high):
+    """References of 2^19 and 2^27 in base 2: the rows are formed again from exact differences.  Scores are whole
+    multiples of 64 x 2^-6 and no sum on the way passes 24 bits, so that they are exact."""
+    B, H, Hkv, n, L = shape
+    if shape is PARTS:
+        _takes_shared_parts(lv, PARTS)
+    g = torch.Generator(device="cuda").manual_seed(16)
+    q = torch.zeros(B, H, n, 64, device="cuda")
+    k = torch.zeros(B, Hkv, L, 64, device="cuda")
+    k[..., 0] = 127 * 64.0                                                   # (block scales of 64)
+    if high == 64.0:
+        q[..., 1:9] = torch.randint(-1, 2, (B, H, n, 8), generator=g, device="cuda") / 64.0
+        k[..., 1:9] = 64.0 * torch.randint(-1, 2, (B, Hkv, L, 8), generator=g, device="cuda")
+    else:
+        k[:, :, ::3, 0] = 126 * 64.0
+    q[..., 0] = high
+    out, want, tol = _cross(lv, "codes", q, k, _randn((B, Hkv, L, 64), 17), 1.0)
+    plain.assert_close(out, want, tol)
