@@ -1090,15 +1090,21 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossArgs a, float unit, flo
   }
   sums[tid >> 4][tid & 15] = x;
   __syncthreads();
-  if (tid >= 8) return;
-  float out[8] = {};
-  for (int s = 0; s < 16; ++s)
+  if (wave != 0) return;
+  float any = 0.f;
+  if (tid < 8) {
+    float out[8] = {};
+    for (int s = 0; s < 16; ++s)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) out[e] += ((const float*)&sums[s][2 * tid])[e];
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+      for (int e = 0; e < 8; ++e) out[e] += ((const float*)&sums[s][2 * tid])[e];
+    const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) out[e] *= inv;
-  store_row<KIND>(a, b, j, r, tid, out);
+    for (int e = 0; e < 8; ++e) { out[e] *= inv; any += out[e]; }
+    store_row<KIND>(a, b, j, r, tid, out);
+  }
+  // (as in store_tile: products that only overflowed under sums that had been let grow, those of all parts together)
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(not_finite(any)) != 0, 0) && l > (float)keys_of(a, b))
+    row_again<KIND>(a, c, b, j, bj, keys_of(a, b), r);
 }
 
 namespace {

@@ -78,6 +78,28 @@ def test_softmax_scale_times_block_scale_leaves_the_range(lv, shape):
     plain.assert_close(out, want, tol)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "codes"])
+@pytest.mark.parametrize("power", [80, 88, 100])
+@pytest.mark.parametrize("shape", SHAPES[4:], ids=str)
+def test_parts_whose_sums_grow_are_joined_without_overflow(lv, shape, power, kind):
+    """Parts of the axis whose first block scores 2^-29 of the rest: products of a part are finite up to V of 2^88, those
+    of all parts together are not."""
+    B, H, Hkv, n, L = shape
+    tiles = B * Hkv * -(-(H // Hkv * n) // 32)
+    parts, rest = divmod(lv.litevar_cross_attn_workspace_bytes(B, H, Hkv, n, L), tiles * 32 * (64 * 4 + 8))
+    assert parts > 4 and rest == 0
+    blocks = -(-L // 64)
+    q, k = 0.1 * _randn((B, H, n, 64), 7), 0.1 * _randn((B, Hkv, L, 64), 8)
+    v = (1 + 0.2 * _randn((B, Hkv, L, 64), 9)) * 2.0 ** power
+    v[..., 1:] *= 2.0 ** -20                                                 # (one dimension ends alone near 2^128)
+    q[..., 0], k[..., 0] = 8.0, 20.125                                       # (a score of 20.125 is 29 in base 2)
+    for p in range(parts):
+        first = 64 * (blocks * p // parts)
+        k[:, :, first:first + 64, 0] = 0
+    out, want, tol = _cross(lv, kind, q, k, v, SM)
+    plain.assert_close(out, want, tol)
+
+
 # 113 tiles of 32 rows in each of two pairs, 82 blocks: the shape that shares K and V in parts in 16 and 8 bits alike
 PARTS = (2, 30, 1, 120, 5200)
 
