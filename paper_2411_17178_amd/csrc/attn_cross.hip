@@ -178,8 +178,9 @@ void k_cross_rows(CrossArgs a, float c) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) { O[0][e] *= alpha; O[1][e] *= alpha; }
     }
+    const float ref = m > -INFINITY ? m : 0.f;           // (only scores of -inf so far)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) S[e] = __builtin_amdgcn_exp2f((S[e] - m) * c);
+    for (int e = 0; e < 16; ++e) S[e] = __builtin_amdgcn_exp2f((S[e] - ref) * c);
     return alpha;
   };
 
@@ -424,7 +425,7 @@ __device__ inline void row_again(const CrossArgs& a, float c, int b, int j, int 
     for (int d = 32; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
     const float to = fmaxf(m, mx);
     const float alpha = m > -INFINITY ? __builtin_amdgcn_exp2f((m - to) * c) : 0.f;
-    const float p = __builtin_amdgcn_exp2f((s - to) * c);
+    const float p = __builtin_amdgcn_exp2f((s - (to > -INFINITY ? to : 0.f)) * c);
     float sum = p;
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
