@@ -456,7 +456,8 @@ litevar_status litevar_windowed_attn_kv8_fwd(const litevar_plan* plan, const voi
  *               litevar_kv8_store; the same lengths), Q and O in bf16.  The codes enter the matrix products exactly, K's
  *               scales multiply fp32 scores, V's fp32 sums or, relative to the largest (at least 2^-96 of it), the
  *               probabilities ahead of their rounding to bf16.
- * Inputs must be finite.  Results do not depend on the run (no atomics).  Asynchronous on `stream`.
+ * Inputs must be finite; a NaN in Q, or in a row of K or V that counts, makes NaN of the results that it enters and of no
+ * others.  Results do not depend on the run (no atomics).  Asynchronous on `stream`.
  */
 litevar_status litevar_cross_attn_workspace_bytes(int32_t B, int32_t H, int32_t H_kv, int32_t q_len, int32_t kv_len,
                                                   size_t* out_bytes);

@@ -178,7 +178,7 @@ void k_cross_rows(CrossArgs a, float c) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) { O[0][e] *= alpha; O[1][e] *= alpha; }
     }
-    const float ref = m > -INFINITY ? m : 0.f;           // (only scores of -inf so far)
+    const float ref = m > -INFINITY ? m : 0.f;           // (only scores of -inf so far, or NaN, which stays)
 #pragma unroll
     for (int e = 0; e < 16; ++e) S[e] = __builtin_amdgcn_exp2f((S[e] - ref) * c);
     return alpha;
@@ -354,6 +354,7 @@ void k_cross_rows(CrossArgs a, float c) {
 
   // ---- join the waves ----
   L += other_half(L);
+  if (not_finite(L)) m = 0.f;                  // (a NaN score enters no maximum: with m = -inf the row would count as one without keys)
   float2* const ML = (float2*)(smem + kWaves * kRows * kPitch * 4);
   __syncthreads();                             // (the rows of V are read)
   float* const mine = (float*)smem + (wave * kRows + n) * kPitch + 4 * hh;
@@ -502,7 +503,7 @@ __device__ inline void keep_part(const CrossArgs& a, int bj, int part, int n_key
     }
   uint64_t bad = far | (__builtin_amdgcn_ballot_w64(not_finite(any)) & (moved | __builtin_amdgcn_ballot_w64(l > (float)n_keys)));
   bad |= bad >> 32;
-  if (lane < 32) a.part_ml[row] = make_float2(n_keys <= 0 ? -INFINITY : (bad >> n) & 1 ? INFINITY : -negm, l);
+  if (lane < 32) a.part_ml[row] = make_float2(n_keys <= 0 ? -INFINITY : (bad >> n) & 1 ? INFINITY : not_finite(l) ? 0.f : -negm, l);
 }
 
 // Many rows: NWV waves of one (batch, kv head), each with 32 rows, share the K and V rows, which pass through LDS in chunks

@@ -1,5 +1,5 @@
-"""Cross attention with scores that fp32 does not hold, in every kernel that a call may take.  Tolerances as in
-test_gpu_cross_attn."""
+"""What is not a number stays visible: a NaN in Q, or in a row of K or V that counts, reaches what the formula makes of it
+in every kernel that a call may take, and nothing else.  Tolerances of what it does not reach as in test_gpu_cross_attn."""
 import pytest
 import torch
 
@@ -23,10 +23,53 @@ def lv():
     return m
 
 
+def _reference(kind, q, k, v):
+    keep = torch.ones(1, 1, 1, k.shape[2], dtype=torch.bool, device="cuda")
+    want, A, S = plain.attention(q, k, v, keep, SM)
+    return want, _tolerance(kind, want, A, S, k.shape[2])
+
+
+def _check(out, want, tol, hit):
+    """hit (broadcast over [B, H, n, 64]): NaN there, right elsewhere."""
+    hit = hit.expand(out.shape)
+    assert bool(torch.isnan(out[hit]).all())
+    plain.assert_close(out[~hit], want[~hit], tol[~hit])
+
+
+def _hit(shape, **where):
+    """Truth values [B, H, n, 64]: batch row 0, the heads of kv head 0, and the row or dimension that is given."""
+    B, H, Hkv, n, L = shape
+    hit = torch.zeros(B, H, n, 64, dtype=torch.bool, device="cuda")
+    hit[0, :where.get("heads", H // Hkv), where.get("row", slice(None)), where.get("dim", slice(None))] = True
+    return hit
+
+
 def _operands(shape, kind):
     B, H, Hkv, n, L = shape
     dtype = torch.float32 if kind == "f32" else torch.bfloat16
     return tuple(_randn(s, i, dtype) for i, s in enumerate([(B, H, n, 64), (B, Hkv, L, 64), (B, Hkv, L, 64)]))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_nan_in_an_operand(lv, shape, kind):
+    B, H, Hkv, n, L = shape
+    q, k, v = _operands(shape, kind)
+    want, tol = _reference(kind, q, k, v)
+    print(f"  nan {kind} {shape}", flush=True)
+
+    def call(name, at):
+        x = dict(q=q, k=k, v=v)
+        x[name] = x[name].clone()
+        x[name][at] = NAN
+        return lv.litevar_cross_attn_fwd(x["q"], x["k"], x["v"], SM)
+    everything, key = (0, 0), L - 70
+    _check(call("k", everything), want, tol, _hit(shape))
+    _check(call("k", (0, 0, key, 5)), want, tol, _hit(shape))
+    _check(call("k", (0, 0, 0)), want, tol, _hit(shape))
+    _check(call("k", (0, 0, slice(L - 50, L))), want, tol, _hit(shape))
+    _check(call("v", (0, 0, key, 5)), want, tol, _hit(shape, dim=5))
+    _check(call("q", (0, 0, n - 1, 5)), want, tol, _hit(shape, heads=1, row=n - 1))
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "codes"])
