@@ -626,7 +626,11 @@ void k_cross_tiles(CrossArgs a, float c) {
   [[maybe_unused]] auto set_scales = [&](float ks, float vs) {
     lane_ks = ks;
     // (a scale of zero belongs to a block of zeros: any will do)
-    lane_lv = vs > 0.f ? fmaxf(log2_of(vs) - log_vmax, -96.f) : 0.f;
+    // (one that is not finite makes NaN of its block's probabilities: it would enter no maximum and no product; as bits, see not_finite)
+    unsigned lv = __float_as_uint(vs > 0.f ? fmaxf(log2_of(vs) - log_vmax, -96.f) : 0.f);
+    lv = not_finite(vs) ? 0x7fc00000u : lv;
+    asm volatile("" : "+v"(lv));
+    lane_lv = __uint_as_float(lv);
     lane_iv = __builtin_amdgcn_exp2f(-lane_lv);
     asm volatile("" : "+v"(lane_ks));          // (its load is waited for here, not wherever the chunks go on)
   };

@@ -99,3 +99,25 @@ def test_scores_below_the_range_of_fp32(lv, shape, kind):
         q0[..., 0] = 0                                                       # (scores of the other keys: exactly these)
         want, A, S = plain.attention(q0, k, v, keep[None, None, None], SM)
         plain.assert_close(out, want, _tolerance(kind, want, A, S, L))
+
+
+@pytest.mark.parametrize("block", [0, 1, -1])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_scales_that_are_not_finite(lv, shape, block):
+    """A NaN scale makes NaN of the rows that read its block, an infinite scale of V nothing that is a number."""
+    B, H, Hkv, n, L = shape
+    q, k, v = _operands(shape, "codes")
+    cache = lv.litevar_kv8_store(lv.litevar_kv8_cache([L], B, Hkv), k, v)
+    k, v = (plain.dequantise(c, s, [L]) for c, s in ((cache.k8, cache.k_scale), (cache.v8, cache.v_scale)))
+    want, tol = _reference("codes", q, k, v)
+    hit = _hit(shape)
+    for name, value in (("k", NAN), ("v", NAN), ("v", INF)):
+        scale = cache.k_scale if name == "k" else cache.v_scale
+        good = scale[0, 0, block].clone()
+        scale[0, 0, block] = value
+        out = lv.litevar_cross_attn_kv8_fwd(q, cache, SM)
+        scale[0, 0, block] = good
+        if value == INF:
+            assert not bool(torch.isfinite(out[hit]).any())
+            out[hit] = NAN
+        _check(out, want, tol, hit)
