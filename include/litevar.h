@@ -394,14 +394,15 @@ litevar_status litevar_windowed_attn_qkv8_fwd(const litevar_plan* plan, const in
  * blocks of LITEVAR_KV8_BLOCK tokens counted from its first; no block spans two segments, so that storing scale by
  * scale gives what storing all of them at once gives.
  *   s = max |x| over the block's rows / 127,   code = clamp(rne(x / s), -127, 127) (0 where s = 0),   value = s * code
- * Both quotients are correctly rounded binary32 quotients.
+ * Both quotients are correctly rounded binary32 quotients.  A block with a value that is not finite has s = NaN, or
+ * infinity where none is NaN, and codes of 0: all its values are NaN.
  *   codes   DEVICE int8 [B, H, L, 64], 16-byte aligned, L = the sum of the segments
  *   scales  DEVICE float [B, H, n_blocks], n_blocks = the sum of ceil(segment / LITEVAR_KV8_BLOCK)
  *   segments, n_segments  HOST, token counts >= 0, at most LITEVAR_MAX_SCALES of them, fewer than 2^31 tokens in all
  *
  * litevar_kv8_blocks  out_first: HOST [n_segments + 1], the first block of every segment, then n_blocks.  Host-only.
  * litevar_kv8_store   quantises the rows of the segments [segment_begin, segment_end) into the cache.
- *     d_k, d_v     DEVICE [B, H, n, 64], n = the tokens of these segments; bf16 or fp32; finite
+ *     d_k, d_v     DEVICE [B, H, n, 64], n = the tokens of these segments; bf16 or fp32
  *     kv_strides   HOST, element strides of the (B, H, token) axes, multiples of 8; NULL = packed
  *     d_len        optional DEVICE int32 [B]: tokens of the row's sequence, counted from the cache's first token, that
  *                  count (taken as at least 0).  Rows from there on are not read, do not enter a scale and leave the cache

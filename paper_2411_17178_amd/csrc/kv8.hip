@@ -89,16 +89,18 @@ __global__ __launch_bounds__(kWaves * 64) void k_kv8_store(StoreArgs a) {
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     if (8 * i < rows) load8<T>(x + min(8 * i + row8, rows - 1) * a.xs[2], v[i]);
-  float mx = 0.f;
+  // (magnitudes compare as integers, in which infinity and NaN are the largest: a block that holds one is left without codes)
+  unsigned top = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     if (8 * i < rows) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) mx = fmaxf(mx, fabsf(v[i][e]));
+      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[i][e]) & 0x7fffffffu);
     }
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
-  const float s = __fdiv_rn(mx, 127.0f);
+  for (int d = 32; d > 0; d >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, d));
+  constexpr unsigned kInf = 0x7f800000u;
+  const float s = top < kInf ? __fdiv_rn(__uint_as_float(top), 127.0f) : 0.f;
   const int64_t row0 = (int64_t)k.bh * a.w.len + k.token;
   int8_t* out = (tensor ? a.codes[1] : a.codes[0]) + (row0 + row8) * 64 + 8 * part;
   // The correctly rounded quotient without a division: x / s by the reciprocal of s, corrected by its exact remainder
@@ -131,7 +133,9 @@ __global__ __launch_bounds__(kWaves * 64) void k_kv8_store(StoreArgs a) {
     }
     if (8 * i + row8 < rows) *(uint2*)(out + 8 * i * 64) = make_uint2(word[0], word[1]);
   }
-  if (lane == 0) (tensor ? a.scale[1] : a.scale[0])[(int64_t)k.bh * a.w.total_blocks + k.index] = s;
+  if (lane == 0)
+    ((unsigned*)(tensor ? a.scale[1] : a.scale[0]))[(int64_t)k.bh * a.w.total_blocks + k.index] =
+        top < kInf ? __float_as_uint(s) : top == kInf ? kInf : 0x7fc00000u;
 }
 
 // Codes -> rows [B][H][len][64] of bf16, or of f16 times the head's power of two (see HeadScales; every wave forms it

@@ -121,3 +121,43 @@ def test_scales_that_are_not_finite(lv, shape, block):
             assert not bool(torch.isfinite(out[hit]).any())
             out[hit] = NAN
         _check(out, want, tol, hit)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("value", [NAN, -NAN, INF, -INF])
+def test_stored_values_that_are_not_finite_show_in_the_scale(lv, value, dtype):
+    """Its block's scale is NaN, or infinite, with codes of zero, so that every value of the block is NaN; other blocks,
+    and rows that do not count, are as without it."""
+    seg, B, H = [5, 130, 64], 2, 3
+    k, v = _randn((B, H, 199, 64), 1, dtype), _randn((B, H, 199, 64), 2, dtype)
+    lens = torch.tensor([199, 100], dtype=torch.int32).cuda()
+    empty = [torch.full((B, H, 199, 64), 55, dtype=torch.int8, device="cuda") for _ in range(2)]
+    clean, cache = (lv.KV8Cache(seg, empty[0].clone(), torch.full((B, H, 5), -5.0, device="cuda"), empty[1].clone(),
+                                torch.full((B, H, 5), -5.0, device="cuda")) for _ in range(2))
+    lv.litevar_kv8_store(clean, k, v, lens=lens)
+    k[0, 1, 5 + 64 + 3, 63] = value                                          # block 2 of batch row 0, head 1
+    v[1, 2, 5 + 10, 0] = value                                               # block 1 of batch row 1, head 2
+    v[1, 0, 150, 7] = value                                                  # behind the length
+    lv.litevar_kv8_store(cache, k, v, lens=lens)
+    for name, b, h, block, rows in (("k", 0, 1, 2, slice(69, 133)), ("v", 1, 2, 1, slice(5, 69))):
+        codes, scale = getattr(cache, name + "8"), getattr(cache, name + "_scale")
+        want_codes, want_scale = getattr(clean, name + "8").clone(), getattr(clean, name + "_scale").clone()
+        assert bool(torch.isnan(scale[b, h, block]) if value != value else scale[b, h, block] == INF)
+        want_codes[b, h, rows] = 0
+        want_scale[b, h, block] = scale[b, h, block]
+        assert torch.equal(codes, want_codes)
+        assert torch.equal(scale.view(torch.int32), want_scale.view(torch.int32))
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_stored_values_that_are_not_finite_reach_the_rows(lv, shape):
+    B, H, Hkv, n, L = shape
+    q, k, v = _operands(shape, "codes")
+    cache = lv.litevar_kv8_store(lv.litevar_kv8_cache([L], B, Hkv), k, v)
+    want, tol = _reference("codes", q, *(plain.dequantise(c, s, [L]) for c, s in ((cache.k8, cache.k_scale), (cache.v8, cache.v_scale))))
+    for value in (NAN, INF):
+        for name in "kv":
+            x = dict(k=k.clone(), v=v.clone())
+            x[name][0, 0, L - 70, 5] = value
+            out = lv.litevar_cross_attn_kv8_fwd(q, lv.litevar_kv8_store(cache, x["k"], x["v"]), SM)
+            _check(out, want, tol, _hit(shape))
