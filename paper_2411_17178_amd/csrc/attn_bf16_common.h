@@ -77,6 +77,13 @@ __device__ inline bool not_finite(float x) {
   return (u & 0x7f800000u) == 0x7f800000u;
 }
 
+// NaN for an infinity, so that a score formed with it is no -inf, which would have no weight
+__device__ inline float nan_unless_finite(float x) {
+  unsigned u = not_finite(x) ? 0x7fc00000u : __float_as_uint(x);
+  asm volatile("" : "+v"(u));                  // (see not_finite)
+  return __uint_as_float(u);
+}
+
 __device__ inline unsigned lds_addr(const void* p) {
   return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
@@ -190,7 +197,7 @@ __device__ inline void attend_row(const AttnArgs& a, float c, int b, int h, int 
     [[maybe_unused]] float v_scale = 1.f;
     if constexpr (KV) {
       const int64_t at = pair * scales.n_blocks + scales.block_of(tok, a.n_scales);
-      k_scale = scales.k[at]; v_scale = scales.v[at];
+      k_scale = nan_unless_finite(scales.k[at]); v_scale = scales.v[at];
     }
     load_half(K + (unsigned)tok * row_bytes, Q8 ? a.k_sz + first_row + tok : nullptr, x, std::integral_constant<bool, Q8 || KV>{}, k_scale);
 #pragma unroll

@@ -110,7 +110,7 @@ __global__ __launch_bounds__(W * 64) void k_attn_kv8(AttnArgs a, KV8Scales ks, i
     uint64_t keep[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) keep[e] = mk[e];
-    if (lane < 32) step_scales[wave][lane] = r.sc;
+    if (lane < 32) step_scales[wave][lane] = make_float2(nan_unless_finite(r.sc.x), r.sc.y);
     asm volatile("" ::: "memory");           // (read by other lanes of the wave; LDS keeps a wave's order)
 
     f32x4 S[2];
