@@ -456,7 +456,8 @@ litevar_status litevar_windowed_attn_kv8_fwd(const litevar_plan* plan, const voi
  * litevar_cross_attn_kv8_fwd: the same with K and V in an 8-bit cache of one segment of kv_len tokens (see
  *               litevar_kv8_store; the same lengths), Q and O in bf16.  The codes enter the matrix products exactly, K's
  *               scales multiply fp32 scores, V's fp32 sums or, relative to the largest (at least 2^-96 of it), the
- *               probabilities ahead of their rounding to bf16.
+ *               probabilities ahead of their rounding to bf16.  A scale that is not finite makes NaN (an infinite one of V:
+ *               infinities or NaN) of the rows that see its block.
  * Inputs must be finite; a NaN in Q, or in a row of K or V that counts, makes NaN of the results that it enters and of no
  * others.  Results do not depend on the run (no atomics).  Asynchronous on `stream`.
  */

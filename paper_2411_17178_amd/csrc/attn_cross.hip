@@ -288,6 +288,7 @@ void k_cross_rows(CrossArgs a, float c) {
         }
       }
       asm volatile("" ::: "memory");           // (the rows of V are read by other lanes than wrote them; LDS keeps a wave's order)
+      [[maybe_unused]] const float ks = CODES ? nan_unless_finite(x.ks) : 1.f;
       f32x16 P[2];                             // codes: the turn's products with V, which the V scale multiplies
       if constexpr (CODES) { P[0] = f32x16{}; P[1] = f32x16{}; }
 #pragma unroll
@@ -308,7 +309,7 @@ void k_cross_rows(CrossArgs a, float c) {
         }
         if constexpr (CODES) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) S[e] *= x.ks;
+          for (int e = 0; e < 16; ++e) S[e] *= ks;
         }
         const float alpha = softmax(S, key0);
         if constexpr (CODES) {
@@ -419,7 +420,7 @@ __device__ inline void row_again(const CrossArgs& a, float c, int b, int j, int 
       for (int e = 0; e < 8; ++e) s = fmaf(x[e], (float)q[d + e], s);
     }
     float vs = 1.f;
-    if constexpr (KIND == kCodes) { s *= a.k_scale[scale_at]; vs = a.v_scale[scale_at]; }
+    if constexpr (KIND == kCodes) { s *= nan_unless_finite(a.k_scale[scale_at]); vs = a.v_scale[scale_at]; }
     s = key0 + lane < n_keys ? s : -INFINITY;
     float mx = s;
 #pragma unroll
@@ -624,7 +625,7 @@ void k_cross_tiles(CrossArgs a, float c) {
     return (int64_t)bj * a.scale_blocks + first_block + min(chunk + lane, n_chunks - 1);
   };
   [[maybe_unused]] auto set_scales = [&](float ks, float vs) {
-    lane_ks = ks;
+    lane_ks = nan_unless_finite(ks);
     // (a scale of zero belongs to a block of zeros: any will do)
     // (one that is not finite makes NaN of its block's probabilities: it would enter no maximum and no product; as bits, see not_finite)
     unsigned lv = __float_as_uint(vs > 0.f ? fmaxf(log2_of(vs) - log_vmax, -96.f) : 0.f);

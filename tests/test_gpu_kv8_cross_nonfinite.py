@@ -104,20 +104,20 @@ def test_scores_below_the_range_of_fp32(lv, shape, kind):
 @pytest.mark.parametrize("block", [0, 1, -1])
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
 def test_scales_that_are_not_finite(lv, shape, block):
-    """A NaN scale makes NaN of the rows that read its block, an infinite scale of V nothing that is a number."""
+    """A NaN scale, or an infinite one of K, makes NaN of the rows that read its block, an infinite one of V no number."""
     B, H, Hkv, n, L = shape
     q, k, v = _operands(shape, "codes")
     cache = lv.litevar_kv8_store(lv.litevar_kv8_cache([L], B, Hkv), k, v)
     k, v = (plain.dequantise(c, s, [L]) for c, s in ((cache.k8, cache.k_scale), (cache.v8, cache.v_scale)))
     want, tol = _reference("codes", q, k, v)
     hit = _hit(shape)
-    for name, value in (("k", NAN), ("v", NAN), ("v", INF)):
+    for name, value in (("k", NAN), ("k", INF), ("v", NAN), ("v", INF)):
         scale = cache.k_scale if name == "k" else cache.v_scale
         good = scale[0, 0, block].clone()
         scale[0, 0, block] = value
         out = lv.litevar_cross_attn_kv8_fwd(q, cache, SM)
         scale[0, 0, block] = good
-        if value == INF:
+        if name == "v" and value == INF:
             assert not bool(torch.isfinite(out[hit]).any())
             out[hit] = NAN
         _check(out, want, tol, hit)
@@ -161,3 +161,16 @@ def test_stored_values_that_are_not_finite_reach_the_rows(lv, shape):
             x[name][0, 0, L - 70, 5] = value
             out = lv.litevar_cross_attn_kv8_fwd(q, lv.litevar_kv8_store(cache, x["k"], x["v"]), SM)
             _check(out, want, tol, _hit(shape))
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_an_infinite_k_scale_under_negative_products(lv, shape):
+    """Every score of the block is -inf: no weight, were the scale not taken for NaN."""
+    B, H, Hkv, n, L = shape
+    q, k, v = _operands(shape, "codes")
+    q, k = -q.abs(), k.abs()
+    cache = lv.litevar_kv8_store(lv.litevar_kv8_cache([L], B, Hkv), k, v)
+    k, v = (plain.dequantise(c, s, [L]) for c, s in ((cache.k8, cache.k_scale), (cache.v8, cache.v_scale)))
+    want, tol = _reference("codes", q, k, v)
+    cache.k_scale[0, 0, 1] = INF
+    _check(lv.litevar_cross_attn_kv8_fwd(q, cache, SM), want, tol, _hit(shape))
