@@ -343,7 +343,7 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
     const unsigned codes_at = base + 16u * (unsigned)lane, to = base + (unsigned)(lane >> 2) * kRingRowBytes;
     u32x4 w;
     asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=v"(w) : "v"(codes_at) : "memory");
-    const float s = ldexpf(scale, v_rows ? v_power : k_power);
+    const float s = ldexpf(nan_unless_finite(scale), v_rows ? v_power : k_power);
     const unsigned w0 = w[0], w1 = w[1], w2 = w[2], w3 = w[3];
     const u32x4 lo = __builtin_bit_cast(u32x4, codes_to_f16(w0, w1, s)), hi = __builtin_bit_cast(u32x4, codes_to_f16(w2, w3, s));
     asm volatile("ds_write_b128 %0, %2\n\tds_write_b128 %1, %3"

@@ -181,7 +181,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_kv8_load(LoadArgs a) {
     HeadScales head;
     for (int i = lane; i < a.w.n_blocks; i += 64) head.add(scales[a.w.first[0] + i]);
     head.join();
-    s = ldexpf(s, head.power());
+    s = ldexpf(nan_unless_finite(s), head.power());
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {

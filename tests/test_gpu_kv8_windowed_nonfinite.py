@@ -61,3 +61,25 @@ def test_a_scale_that_is_not_finite_stays_in_its_rows(lv, route, B, H, name, sto
         assert not bool(torch.isfinite(out[hit]).any())
         if value != value or stored:
             assert bool(torch.isnan(out[hit]).all())
+
+
+@pytest.mark.parametrize("route,B,H", ALL, ids=str)
+def test_an_infinite_k_scale_under_negative_products(lv, route, B, H):
+    """Every score of the block is -inf: no weight, were the scale not taken for NaN."""
+    q_scales, waves = route
+    plan = lv.litevar_mask_build(VAR256, 1, None, 0, q_scales, waves_per_group=waves)
+    mask = lv.litevar_mask_export_dense(plan)[0].bool()
+    g = torch.Generator(device="cuda").manual_seed(22)
+    q = -torch.randn(B, H, plan.q_len, 64, generator=g, device="cuda").abs().to(torch.bfloat16)
+    k, v = (torch.randn(B, H, 680, 64, generator=g, device="cuda") for _ in range(2))
+    cache = lv.litevar_kv8_store(lv.litevar_kv8_cache([s * s for s in VAR256], B, H), k.abs() + 0.5, v)
+    want, A, S, floor = _reference(cache, q, mask)
+    tol = _tolerance(A, S, floor)
+    scale = (10 if q_scales is None else q_scales[1]) - 1
+    lo = cache.offsets[scale]
+    cache.k_scale[0, 1, cache.first_block[scale]] = INF
+    out = lv.litevar_windowed_attn_kv8_fwd(plan, q, cache, SM)
+    hit = torch.zeros(B, H, plan.q_len, dtype=torch.bool, device="cuda")
+    hit[0, 1] = mask[:, lo:min(lo + 64, cache.offsets[scale + 1])].any(-1)
+    plain.assert_close(out[~hit], want[~hit], tol[~hit])
+    assert bool(torch.isnan(out[hit]).all())
