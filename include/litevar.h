@@ -418,7 +418,7 @@ litevar_status litevar_windowed_attn_qkv8_fwd(const litevar_plan* plan, const in
  *                     form the products in f16: s * code off by 2^-11 relative at most, a weight by 2^-10 relative or
  *                     2^-21 of the row's sum (as exact as the others where a head's block scales differ by more than
  *                     2^20, but by a slow path).  Other plans form them from the codes, exactly, and round a weight
- *                     times its V scale to bf16.  A scale that is not finite reaches the queries that keep one of its
+ *                     times its V scale to bf16 (results below 2^-100 are formed in fp32).  A scale that is not finite reaches the queries that keep one of its
  *                     block's tokens and no others.  Other arguments as litevar_windowed_attn_fwd.
  * All but litevar_kv8_blocks and the workspace size: asynchronous on `stream`.
  */

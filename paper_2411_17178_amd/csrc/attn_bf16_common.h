@@ -248,6 +248,18 @@ __device__ inline void attend_row(const AttnArgs& a, float c, int b, int h, int 
   if (shared) op[(a.B / 2) * a.os[0]] = r;
 }
 
+// The keys of query `column` of a patch of 16 for attend_row, in the patch's steps.
+struct PatchKeys {
+  const AttnArgs& a;
+  int64_t step0; int n_blocks, column;
+  __device__ bool key(int block, int i, int& tok) const {
+    const int64_t s = step0 + block;
+    const int r = i & 15;
+    tok = a.step_tok[s * kStepKeys + i];
+    return (a.step_mask[s * 8 + 4 * (i >> 4) + (r & 3)] >> ((r >> 2) * 16 + column)) & 1;
+  }
+};
+
 // Which of a query's 32 values in this lane (r: pairs of bf16, dims 32 dt + 8 j + 4 (lane / 32) .. + 3 of a 32 x 32 tile's
 // column, in that order) are not finite.
 __device__ inline unsigned not_finite_dims(const unsigned (&r)[2][8]) {

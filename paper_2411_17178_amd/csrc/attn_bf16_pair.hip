@@ -168,10 +168,8 @@ struct PatchState {       // one query patch of a wave
 
 // The keys of one query for attend_row, in the steps of the patch of 16 that holds the query's row, one of the group's
 // sixteen from `patches` on
-struct StepKeys {
-  const AttnArgs& a;
-  int64_t step0; int n_blocks, column;
-  __device__ StepKeys(const AttnArgs& args, const WaveDesc* patches, int qrow) : a(args), step0(0), n_blocks(0), column(0) {
+struct StepKeys : PatchKeys {
+  __device__ StepKeys(const AttnArgs& args, const WaveDesc* patches, int qrow) : PatchKeys{args, 0, 0, 0} {
     const WaveDesc wd = patches[lane_of_wave() & (kGroupPatches - 1)];
     const int d = qrow - wd.q_base, dy = d / max((int)wd.sk, 1), dx = d - dy * wd.sk;
     const bool holds = d >= 0 && dy < kPatch && dx < kPatch && ((wd.valid >> (kPatch * dy + dx)) & 1u);
@@ -181,12 +179,6 @@ struct StepKeys {
     step0 = __builtin_amdgcn_readlane(wd.step_begin, at);
     n_blocks = __builtin_amdgcn_readlane(wd.n_steps, at);
     column = __builtin_amdgcn_readlane(kPatch * dy + dx, at);
-  }
-  __device__ bool key(int block, int i, int& tok) const {
-    const int64_t s = step0 + block;
-    const int r = i & 15;
-    tok = a.step_tok[s * kStepKeys + i];
-    return (a.step_mask[s * 8 + 4 * (i >> 4) + (r & 3)] >> ((r >> 2) * 16 + column)) & 1;
   }
 };
 

@@ -202,16 +202,34 @@ __global__ __launch_bounds__(W * 64) void k_attn_kv8(AttnArgs a, KV8Scales ks, i
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) acc[p] = f32x4{O[0][p], O[1][p], O[2][p], O[3][p]};
   }
-  if (qrow < 0) return;
   const float inv = 1.f / sum;
-  __bf16* o = (__bf16*)a.o + b * a.os[0] + h * a.os[1] + qrow * a.os[2] + 16 * g4 + 4 * kPieces * wave;
+  float largest = 0.f;                         // magnitude of the row's results that this wave stores
 #pragma unroll
-  for (int p = 0; p < kPieces; ++p) {
-    bf16x4 r;
+  for (int p = 0; p < kPieces; ++p)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] = (__bf16)(acc[p][e] * inv);
-    *(bf16x4*)(o + 4 * p) = r;
-    if (shared) *(bf16x4*)(o + 4 * p + (a.B / 2) * a.os[0]) = r;
+    for (int e = 0; e < 4; ++e) { acc[p][e] *= inv; largest = fmaxf(largest, fabsf(acc[p][e])); }
+  if (qrow >= 0) {
+    __bf16* o = (__bf16*)a.o + b * a.os[0] + h * a.os[1] + qrow * a.os[2] + 16 * g4 + 4 * kPieces * wave;
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+      bf16x4 r;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r[e] = (__bf16)acc[p][e];
+      *(bf16x4*)(o + 4 * p) = r;
+      if (shared) *(bf16x4*)(o + 4 * p + (a.B / 2) * a.os[0]) = r;
+    }
+  }
+  // Rows of very small values are formed again in fp32: products of weights and V scales below 2^-126 have lost bits as bf16
+  const bool small = qrow >= 0 && largest > 0.f && largest < 0x1p-100f;
+  uint64_t again = __builtin_amdgcn_ballot_w64(small);
+  if (__builtin_expect(again != 0, 0)) {
+    again = (again | (again >> 16) | (again >> 32) | (again >> 48)) & 0xffffull;
+    for (; again != 0; again &= again - 1) {
+      wait_vmcnt<0>();                         // (what is stored next goes to places that were just stored to)
+      const int at = __builtin_ctzll(again), l0 = lane_of_wave();
+      attend_row<false, true>(a, c, b, h, __builtin_amdgcn_readlane(qrow, at), shared, W == 1 || ((l0 >> 2) & 3) == wave,
+                              PatchKeys{a, S0, n_steps, at}, ks);
+    }
   }
 }
 
