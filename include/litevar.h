@@ -415,8 +415,8 @@ litevar_status litevar_windowed_attn_qkv8_fwd(const litevar_plan* plan, const in
  *                     strides as there; d_workspace DEVICE, 256-byte aligned, at least
  *                     litevar_windowed_attn_kv8_workspace_bytes() bytes (NULL where that is 0), contents undefined
  *                     before and after; calls that share a workspace must not overlap.  Plans of 16 patches per group
- *                     form the products in f16: s * code off by 2^-11 relative at most, a weight by 2^-10 relative or
- *                     2^-21 of the row's sum (as exact as the others where a head's block scales differ by more than
+ *                     form the products in f16: s * code off by 2^-11 relative at most, a weight, towards zero, by 2^-10
+ *                     relative or 2^-25 of the row's sum (as exact as the others where a head's block scales differ by more than
  *                     2^20, but by a slow path).  Other plans form them from the codes, exactly, and round a weight
  *                     times its V scale to bf16 (results below 2^-100 are formed in fp32).  A scale that is not finite reaches the queries that keep one of its
  *                     block's tokens and no others.  Other arguments as litevar_windowed_attn_fwd.

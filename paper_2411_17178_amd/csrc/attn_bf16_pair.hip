@@ -202,7 +202,7 @@ struct StepKeys : PatchKeys {
 // power of two that puts its largest block scale near 2^7 (values below 2^14), V's likewise, every query by its own; the
 // powers leave through the softmax scale of the lane and the stored result.  f16 holds three bits more than bf16: a code
 // times its scale is off by 2^-11 at most, a probability by 2^-10 (towards zero, in the sum and the products alike; weights
-// below 2^-11 of the row's sum by up to 2^-21 of it, where f16 is subnormal).  With bf16 in their place the result was off by 0.0033
+// below 2^-15 of the row's sum by up to 2^-25 of it, where f16 is subnormal).  With bf16 in their place the result was off by 0.0033
 // relative to its norm, by 0.0017 so, most of it the rounding of the stored result.  Heads whose block scales differ by more than 2^20
 // would lose bits of the smaller blocks: all their rows are formed again from the codes.
 //   KV = 1: K and V are copies in f16 (k_kv8_load), which come by LDS-DMA.
@@ -216,7 +216,12 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
   static_assert(KV == 0 || (PW == 2 && !Q8), "the cache's forms have wide patches");
   constexpr bool CODES = Q8 || KV == 2;            // K and V come through registers
   using E8 = std::conditional_t<KV != 0, f16x8, bf16x8>;
-  [[maybe_unused]] constexpr float kMost = KV ? 0x1p15f : kMostSum, kLeast = KV ? 0x1p-3f : kLeastSum;
+  [[maybe_unused]] constexpr float kMost = KV ? 65000.f : kMostSum, kLeast = KV ? 0x1p1f : kLeastSum;
+  // KV: a row's sum is kept between 2 and 65 000 in each lane (f16 ends at 65 504, so that a weight that does not fit shows in the
+  // sum), and the reference lies 2^3 below 0 or the largest score: the last bit of a weight, 2^-24, is 2^-25 of the sum at
+  // most.  (From sums of 2^-3 on, 16 639 weights of 2^-21 beside a large one counted as zero, 0.7 % of the row.  2^4
+  // below: scores of standard deviation 6 move the reference more often, 2240 tokens, 288 pairs 242 us; so 232, without 226.)
+  [[maybe_unused]] constexpr float kBase = KV ? 3.f : 0.f;
   constexpr bool WIDE = PW == 2;                   // the group's wide patches (32 queries), else its patches (16)
   constexpr int C = kDmaKeys;
   constexpr int R = kRingChunks * C;               // ring slots
@@ -537,7 +542,7 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
   [[maybe_unused]] const bool band = (pw.sk_ny & 0xffff) == 0;
   [[maybe_unused]] const float slack = kSlack / c;
   [[maybe_unused]] bf16x8 ones;
-  ps.negm = 0.f;
+  ps.negm = kBase;
   if constexpr (WIDE) {
     ps.L = 0.f; ps.unset = queries; ps.far = 0;
     const int nx = pw.nx_kq & 0xffff, ny = pw.sk_ny >> 16, dy = (n * pw.magic) >> 16, dx = n - dy * nx;
@@ -773,7 +778,7 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
       const float now = sum + other_half(sum), before = ps.L + other_half(ps.L);
       float to = mx > -INFINITY ? __builtin_fmaf(mx, cs, ps.negm) : kFloor;
       if (before > 0.f) to = fmaxf(to, __builtin_amdgcn_logf(before));         // (base 2)
-      const float shift = (now > kMost || now < kLeast) && to > kFloor ? rintf(to) : 0.f;
+      const float shift = (now > kMost || now < kLeast) && to > kFloor ? rintf(to) - kBase : 0.f;
       const float alpha = before > 0.f ? __builtin_amdgcn_exp2f(-shift) : 1.f;
       ps.negm -= shift; ps.L *= alpha;
       ps.far |= is_far(ps.negm);
@@ -870,7 +875,7 @@ void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV 
     const float sum = ps.L + other_half(ps.L);
     float inv = 1.f / sum;
     if constexpr (KV != 0) {
-      // V's power of two, with the division where both together are a normal number (the sum is between 2^-3 and 2^27)
+      // V's power of two, with the division where both together are a normal number (the sum is between 2 and 2^27)
       if (__builtin_expect(v_power > -90 && v_power < 90, 1)) {
         inv = ldexpf(inv, -v_power);
       } else {

@@ -45,3 +45,24 @@ def test_v_near_the_ends_of_its_range(lv, route, B, H, power, some):
     v[:, :, 424 + 64:424 + 128] *= some
     v[:, :, 5:14] *= some
     _run(lv, route, k, v * 2.0 ** power, q)
+
+
+@pytest.mark.parametrize("side", [16, 32], ids=["in_the_kernel", "through_a_copy"])
+def test_long_flat_tails_keep_their_weight(lv, side):
+    """One key with nearly all the weight, 16 639 of 2^-21 of it each, in a row's first steps or in its last: the tail's sum
+    is 0.7 %, and all of the result.  A weight is off by its f16's last bit, 2^-24, over a row's sum of at least 2, so that
+    the result of n keys of |v| <= 1 is off by 2^-25 (n + n |out|) <= 2^-24 n besides the relative roundings."""
+    scales = (128, side)
+    n = 128 * 128 + side * side
+    plan = lv.litevar_mask_build(scales, -1, None, 0, (1, 2), waves_per_group=16)
+    assert (lv.litevar_windowed_attn_kv8_workspace_bytes(plan, 1, 1) > 0) == (side == 32)
+    for sink in (0, 5000, n - 1):
+        q, k, v = torch.zeros(1, 1, side * side, 64, device="cuda"), torch.zeros(1, 1, n, 64, device="cuda"), torch.ones(1, 1, n, 64, device="cuda")
+        q[..., 0], k[..., 0] = 8.0, -16.67                                   # (scores: 2^-24.05, and 2^-2.8)
+        k[:, :, sink, 0], v[:, :, sink] = -1.97, 0
+        cache = lv.litevar_kv8_store(lv.litevar_kv8_cache([s * s for s in scales], 1, 1), k, v)
+        q = q.to(torch.bfloat16)
+        out = lv.litevar_windowed_attn_kv8_fwd(plan, q, cache, SM)
+        want, A, S, _ = _reference(cache, q, torch.ones(side * side, n, dtype=torch.bool, device="cuda"))
+        assert 0.005 < want.min().item() <= want.max().item() < 0.01
+        plain.assert_close(out, want, (3.25 * plain.U + 2 * torch.expm1(2.0 ** -11 * S)) * A + 2.0 ** -24 * n)
