@@ -452,7 +452,8 @@ litevar_status litevar_windowed_attn_kv8_fwd(const litevar_plan* plan, const voi
  *   d_kv_len    optional DEVICE int32 [B], taken as at least 0 and at most kv_len; NULL: kv_len for all.  K and V rows
  *               from there on are not read.
  *   d_workspace DEVICE, 16-byte aligned, at least litevar_cross_attn_workspace_bytes() bytes (NULL where that is 0),
- *               contents undefined before and after; calls that share a workspace must not overlap
+ *               contents undefined before and after; calls that share a workspace must not overlap.  The size is that of
+ *               the same call in any type, and does not grow with q_len or kv_len throughout: ask for every shape
  * litevar_cross_attn_kv8_fwd: the same with K and V in an 8-bit cache of one segment of kv_len tokens (see
  *               litevar_kv8_store; the same lengths), Q and O in bf16.  The codes enter the matrix products exactly, K's
  *               scales multiply fp32 scores, V's fp32 sums or, relative to the largest (at least 2^-96 of it), the

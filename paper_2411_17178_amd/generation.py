@@ -83,10 +83,15 @@ class GenerationLayer:
         return binding.litevar_windowed_attn_kv8_fwd(self.plans[k], q_k, cache, sm_scale, out=out_k, cfg_share=share,
                                                      workspace=workspace, stream=stream)
 
+    def cross_workspace_bytes(self, B, H, H_kv, states_len):
+        """Bytes of the workspace that cross needs at most, whichever the step (the last step may need less than one before it)."""
+        return max(binding.litevar_cross_attn_workspace_bytes(B, H, H_kv, s * s, states_len) for s in self.scales)
+
     @staticmethod
     def cross(q_k, states, sm_scale, lens=None, out_k=None, workspace=None, stream=None):
         """A conditioned layer's attention of `q_k` [B, H, n, 64] to an encoder's states, the same at every step:
-        `states` is a pair (k, v) [B, H_kv, len, 64] or an 8-bit cache of one segment."""
+        `states` is a pair (k, v) [B, H_kv, len, 64] or an 8-bit cache of one segment.  `workspace`: a uint8 CUDA tensor
+        of cross_workspace_bytes() bytes (allocated per call when omitted)."""
         if isinstance(states, binding.KV8Cache):
             return binding.litevar_cross_attn_kv8_fwd(q_k, states, sm_scale, lens=lens, out=out_k, workspace=workspace, stream=stream)
         return binding.litevar_cross_attn_fwd(q_k, states[0], states[1], sm_scale, lens=lens, out=out_k, workspace=workspace,
