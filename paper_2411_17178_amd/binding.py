@@ -647,6 +647,7 @@ def litevar_windowed_attn_kv8_fwd(plan, q, cache, sm_scale, out=None, cfg_share=
         with context:
             return litevar_windowed_attn_kv8_fwd(plan, q, cache, sm_scale, out, cfg_share, workspace)
     handle = plan.handle
+    assert plan.blob is None or plan.blob.device == device, "the plan lies on another device than q"
     if q.dtype != torch.bfloat16:
         raise TypeError(f"unsupported dtype {q.dtype}")
     B, H, Lq, D = shape = q.shape
