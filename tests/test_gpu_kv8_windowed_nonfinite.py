@@ -83,3 +83,22 @@ def test_an_infinite_k_scale_under_negative_products(lv, route, B, H):
     hit[0, 1] = mask[:, lo:min(lo + 64, cache.offsets[scale + 1])].any(-1)
     plain.assert_close(out[~hit], want[~hit], tol[~hit])
     assert bool(torch.isnan(out[hit]).all())
+
+
+@pytest.mark.parametrize("route,B,H", ALL, ids=str)
+@pytest.mark.parametrize("whole", [False, True])
+def test_a_query_of_nan_stays_in_its_row(lv, route, B, H, whole):
+    q_scales, waves = route
+    plan = lv.litevar_mask_build(VAR256, 2, None, 0, q_scales, waves_per_group=waves)
+    cache = _cache(lv, VAR256, B, H, 5)
+    g = torch.Generator(device="cuda").manual_seed(23)
+    q = torch.randn(B, H, plan.q_len, 64, generator=g, device="cuda").to(torch.bfloat16)
+    want, A, S, floor = _reference(cache, q, lv.litevar_mask_export_dense(plan)[0].bool())
+    tol = _tolerance(A, S, floor)
+    for i in (0, plan.q_len - 1):
+        bad = q.clone()
+        bad[0, 1, i, slice(None) if whole else 7] = NAN
+        out = lv.litevar_windowed_attn_kv8_fwd(plan, bad, cache, SM)
+        assert bool(torch.isnan(out[0, 1, i]).all())
+        out[0, 1, i] = want[0, 1, i].to(torch.bfloat16)
+        plain.assert_close(out, want, tol)
