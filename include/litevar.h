@@ -398,11 +398,11 @@ litevar_status litevar_windowed_attn_qkv8_fwd(const litevar_plan* plan, const in
  * infinity where none is NaN, and codes of 0: all its values are NaN.
  *   codes   DEVICE int8 [B, H, L, 64], 16-byte aligned, L = the sum of the segments
  *   scales  DEVICE float [B, H, n_blocks], n_blocks = the sum of ceil(segment / LITEVAR_KV8_BLOCK)
- *   segments, n_segments  HOST, token counts >= 0, at most LITEVAR_MAX_SCALES of them, fewer than 2^31 tokens in all
+ *   segments, n_segments  HOST, token counts >= 0, at most LITEVAR_MAX_SCALES of them, fewer than 2^31 - 64 tokens in all
  *
  * litevar_kv8_blocks  out_first: HOST [n_segments + 1], the first block of every segment, then n_blocks.  Host-only.
  * litevar_kv8_store   quantises the rows of the segments [segment_begin, segment_end) into the cache.
- *     d_k, d_v     DEVICE [B, H, n, 64], n = the tokens of these segments; bf16 or fp32
+ *     d_k, d_v     DEVICE [B, H, n, 64], n = the tokens of these segments; bf16 or fp32, 16-byte aligned
  *     kv_strides   HOST, element strides of the (B, H, token) axes, multiples of 8; NULL = packed
  *     d_len        optional DEVICE int32 [B]: tokens of the row's sequence, counted from the cache's first token, that
  *                  count (taken as at least 0).  Rows from there on are not read, do not enter a scale and leave the cache
@@ -415,11 +415,14 @@ litevar_status litevar_windowed_attn_qkv8_fwd(const litevar_plan* plan, const in
  *                     strides as there; d_workspace DEVICE, 256-byte aligned, at least
  *                     litevar_windowed_attn_kv8_workspace_bytes() bytes (NULL where that is 0), contents undefined
  *                     before and after; calls that share a workspace must not overlap.  Plans of 16 patches per group
- *                     form the products in f16: s * code off by 2^-11 relative at most, a weight, towards zero, by 2^-10
- *                     relative or 2^-25 of the row's sum (as exact as the others where a head's block scales differ by more than
- *                     2^20, but by a slow path).  Other plans form them from the codes, exactly, and round a weight
- *                     times its V scale to bf16 (results below 2^-100 are formed in fp32).  A scale that is not finite reaches the queries that keep one of its
- *                     block's tokens and no others.  Other arguments as litevar_windowed_attn_fwd.
+ *                     (patches_per_wave other than 1) form the products in f16: s * code off by 2^-11 relative at most, a
+ *                     weight, towards zero, by 2^-10 relative or 2^-25 of the row's sum (as exact as the others where a
+ *                     head's block scales differ by more than 2^20, but by a slow path).  Other plans form them from the
+ *                     codes, exactly (|q| below 2^114: sums of q times a code are held in fp32), and round a weight
+ *                     times its V scale to bf16 (results below 2^-100 are formed in fp32).  A scale that is not finite
+ *                     reaches the queries that keep one of its block's tokens and no others.  Plans that keep every
+ *                     pair have no kernel of their own here, as they have for litevar_windowed_attn_fwd.  Other
+ *                     arguments as litevar_windowed_attn_fwd.
  * All but litevar_kv8_blocks and the workspace size: asynchronous on `stream`.
  */
 #define LITEVAR_KV8_BLOCK 64
@@ -444,10 +447,11 @@ litevar_status litevar_windowed_attn_kv8_fwd(const litevar_plan* plan, const voi
  * Cross attention to an encoder's states, which a conditioned model of this kind has behind the self attention of every
  * layer (no part of the paper's method):
  *   O[b, h, i] = sum over t < len[b] of softmax_t(sm_scale * q_i . k_t) v_t,   zeros where len[b] = 0.
- *   d_q, d_o    DEVICE [B, H, q_len, 64]; d_k, d_v DEVICE [B, H_kv, kv_len, 64], H a multiple of H_kv: query head h reads
- *               kv head h / (H / H_kv).  q_len and kv_len may be 0 (K and V may then be NULL).  d_o must not overlap
+ *   d_q, d_o    DEVICE [B, H, q_len, 64]; d_k, d_v DEVICE [B, H_kv, kv_len, 64], all 16-byte aligned, H a multiple of H_kv:
+ *               query head h reads kv head h / (H / H_kv).  q_len and kv_len may be 0 (K and V may then be NULL).  d_o must not overlap
  *               the inputs.
  *   dt          BF16: bf16 MFMA with fp32 accumulation, probabilities rounded to bf16 before P V.  F32: fp32 throughout.
+ *   sm_scale    finite, positive, at most 1e4
  *   strides     HOST, element strides of the (B, head, token) axes, multiples of 8, token stride >= 64; NULL = packed
  *   d_kv_len    optional DEVICE int32 [B], taken as at least 0 and at most kv_len; NULL: kv_len for all.  K and V rows
  *               from there on are not read.
@@ -455,7 +459,7 @@ litevar_status litevar_windowed_attn_kv8_fwd(const litevar_plan* plan, const voi
  *               contents undefined before and after; calls that share a workspace must not overlap.  The size is that of
  *               the same call in any type, and does not grow with q_len or kv_len throughout: ask for every shape
  * litevar_cross_attn_kv8_fwd: the same with K and V in an 8-bit cache of one segment of kv_len tokens (see
- *               litevar_kv8_store; the same lengths), Q and O in bf16.  The codes enter the matrix products exactly, K's
+ *               litevar_kv8_store; the same lengths), Q and O in bf16.  The codes enter the matrix products exactly (|q| below 2^114), K's
  *               scales multiply fp32 scores, V's fp32 sums or, relative to the largest (at least 2^-96 of it), the
  *               probabilities ahead of their rounding to bf16.  A scale that is not finite makes NaN (an infinite one of V:
  *               infinities or NaN) of the rows that see its block.

@@ -154,7 +154,7 @@ template <class E8> struct WidePatchState {   // a wave's 32 queries
   E8 q[4];                // Q^T as the B operand: lane (n, h) holds Q[query n][16 t + 8 h .. + 7]
   f32x16 O[2];            // O^T accumulators: dims 32 dt + 8 (e / 4) + 4 h + e % 4 of query n
   float L, negm;          // this lane's part of the row sum, minus the softmax reference m (base 2, whole numbers)
-  uint64_t unset;         // lanes whose query's sum is still below kLeastSum
+  uint64_t unset;         // lanes whose query's sum is still below kLeastSum (KV: kLeast)
   uint64_t far;           // lanes whose reference was beyond kFarReference at some time
   bf16x8 b;               // B operand of the mask product, see run_step32
 };
@@ -214,7 +214,7 @@ template <int PW, bool Q8, int KV = 0>
 __global__ __launch_bounds__((kGroupPatches / PW) * 64) __attribute__((amdgpu_waves_per_eu(4, 4)))
 void k_attn_bf16_pair(AttnArgs a, WideArgs wide, float c, std::conditional_t<KV != 0, KV8Scales, NoScales> scales) {
   static_assert(KV == 0 || (PW == 2 && !Q8), "the cache's forms have wide patches");
-  constexpr bool CODES = Q8 || KV == 2;            // K and V come through registers
+  constexpr bool CODES = Q8 || KV == 2;            // K and V come as codes (Q8: through registers, KV: by LDS-DMA)
   using E8 = std::conditional_t<KV != 0, f16x8, bf16x8>;
   [[maybe_unused]] constexpr float kMost = KV ? 65000.f : kMostSum, kLeast = KV ? 0x1p1f : kLeastSum;
   // KV: a row's sum is kept between 2 and 65 000 in each lane (f16 ends at 65 504, so that a weight that does not fit shows in the

@@ -514,7 +514,7 @@ __device__ inline void keep_part(const CrossArgs& a, int bj, int part, int n_key
 //
 // Softmax in base 2: the reference is the largest score of the first block and moves (by whole powers of two) when a sum
 // passes 2^40, so that no maximum is formed in the other blocks.  Rows whose reference went beyond kFarReference, where its
-// rounding would show, and rows that overflowed are formed again behind the store.
+// rounding would show (on codes kFarCodes, for the V scale that joins it), and rows that overflowed are formed again behind the store.
 //
 // Codes come to a place behind the buffers and are converted (exactly) from there by the wave that brought them.  Two buffers
 // do, 40 KiB with the codes, so that a CU holds four workgroups of four waves or two of eight; it costs the score products
@@ -1122,7 +1122,8 @@ namespace {
 // CU there is nothing to gain.  (Tiles, rows, blocks), bf16, us without / with as many parts as given here: (1, 1, 64) 26.2 / 8.7 (64);
 // (8, 256, 64) 27.9 / 10.4 (18); (32, 1024, 64) 31.4 / 13.4 (9); (128, 4096, 64) 36.5 / 25.6 (4); (128, 4096, 256) 124 / 56 (4);
 // (192, 4992, 165) 80 / 58 (5); (200, 6000, 125) 64 / 50 (5); (260, 5200, 94) 62 / 56 (3); (300, 9600, 125) 91 / 86 (3);
-// declined: (256, 8192, 188) 118 / 100 (4), fp32 257 / 285; (220, 7040, 63) 35.6 / 38.1 (3); (400, 12800, 157) 117 / 155 (2); (64, 64, 4) 5.8 / 7.9 (4); (256, 256, 64) 40.2 / 46.2 (4); (256, 6400, 64) 39.7 / 41.4 (4).
+// declined (one rule for all types, which the size of the workspace knows nothing of: 225 to 256 tiles for fp32's sake): (256, 8192,
+// 188) 118 / 100 (4), fp32 257 / 285; (220, 7040, 63) 35.6 / 38.1 (3); (400, 12800, 157) 117 / 155 (2); (64, 64, 4) 5.8 / 7.9 (4); (256, 256, 64) 40.2 / 46.2 (4); (256, 6400, 64) 39.7 / 41.4 (4).
 int parts_of(int64_t tiles, int64_t rows, int64_t kv_len) {
   const int64_t blocks = (kv_len + kBlock - 1) / kBlock;
   const bool long_axis = blocks >= 80;

@@ -122,7 +122,7 @@ struct KV8Scales {
 #endif
 };
 
-// in_kernel: the codes are converted on their way into LDS; else a.k and a.v are copies that launch_kv8_copy made
+// in_kernel: the codes are converted on their way into LDS; else a.k and a.v are the f16 copies that k_kv8_load<true> made
 litevar_status launch_attn_kv8_pair(const litevar_plan* pl, const AttnArgs& a, const KV8Scales& scales, bool in_kernel, hipStream_t st);
 litevar_status launch_attn_kv8(const litevar_plan* pl, const AttnArgs& a, const KV8Scales& scales, hipStream_t st);
 litevar_status launch_attn_f32(const litevar_plan* pl, const AttnArgs& a, hipStream_t st);

@@ -147,6 +147,10 @@ def test_stored_values_that_are_not_finite_show_in_the_scale(lv, value, dtype):
         want_scale[b, h, block] = scale[b, h, block]
         assert torch.equal(codes, want_codes)
         assert torch.equal(scale.view(torch.int32), want_scale.view(torch.int32))
+    for loaded, sound, (b, h, rows) in zip(lv.litevar_kv8_load(cache), lv.litevar_kv8_load(clean), ((0, 1, slice(69, 133)), (1, 2, slice(5, 69)))):
+        assert bool(torch.isnan(loaded[b, h, rows]).all())
+        loaded[b, h, rows] = sound[b, h, rows]
+        assert torch.equal(loaded.view(torch.int16), sound.view(torch.int16))
 
 
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
