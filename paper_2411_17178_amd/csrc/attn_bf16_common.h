@@ -388,7 +388,15 @@ __device__ inline void read_v(const unsigned (&v)[2], u32x2 (&va)[8]) {
                : "v"(v[0]), "v"(v[1]), "i"(AT), "i"(AT + 8 * kRow), "i"(AT + 16 * kRow), "i"(AT + 24 * kRow) : "memory");
 }
 
-// ---- 8-bit cache in f16 ----
+// ---- 8-bit cache ----
+// eight codes (a word pair) as bf16, exactly
+__device__ inline bf16x8 codes_to_bf16(unsigned lo, unsigned hi) {
+  bf16x8 r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = (__bf16)(float)((int)((e < 4 ? lo : hi) << (24 - 8 * (e & 3))) >> 24);
+  return r;
+}
+
 // The power of two that brings x to [2^13, 2^14).
 __device__ inline int power_to_14(float x) { return x > 0.f ? 14 - __builtin_amdgcn_frexp_expf(x) : 0; }
 

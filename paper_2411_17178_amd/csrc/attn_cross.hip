@@ -84,14 +84,6 @@ __device__ inline float log2_of(float x) {
   return x < 0x1p-126f ? __builtin_amdgcn_logf(x * 0x1p24f) - 24.f : __builtin_amdgcn_logf(x);
 }
 
-// eight codes (a word pair) as bf16, exactly
-__device__ inline bf16x8 codes_to_bf16(unsigned lo, unsigned hi) {
-  bf16x8 r;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = (__bf16)(float)((int)((e < 4 ? lo : hi) << (24 - 8 * (e & 3))) >> 24);
-  return r;
-}
-
 // Writes eight output values of row r, dims 8 part .. + 7.
 template <int KIND> __device__ inline void store_row(const CrossArgs& a, int b, int j, int r, int part, const float (&x)[8]) {
   const Row w = row_at(a, j, r);
@@ -1178,15 +1170,6 @@ int64_t tiles_of(int32_t B, int32_t H, int32_t H_kv, int32_t q_len) {
   return (int64_t)B * H_kv * (((int64_t)(H / H_kv) * q_len + kRows - 1) / kRows);
 }
 
-// (the stride of an axis with one entry is never used, and is what it is)
-litevar_status strides_of(const int64_t* s, int B, int heads, int64_t n, int D, int64_t (&out)[3]) {
-  if (!s) { out[2] = D; out[1] = n * D; out[0] = heads * n * D; return LITEVAR_OK; }
-  out[0] = B > 1 ? s[0] : 0; out[1] = heads > 1 ? s[1] : 0; out[2] = n > 1 ? s[2] : D;
-  if (out[2] < D || out[2] % 8 || out[1] < 0 || out[0] < 0 || out[1] % 8 || out[0] % 8)
-    return fail(LITEVAR_E_INVALID_ARG, "strides must be non-negative multiples of 8 with token stride >= D");
-  return LITEVAR_OK;
-}
-
 template <int KIND> litevar_status launch(CrossArgs& a, float c, hipStream_t st) {
   const int64_t tiles = (int64_t)a.B * a.Hkv * a.tiles;
   auto join_parts = [&](float unit) {
@@ -1248,9 +1231,9 @@ litevar_status cross_attention(CrossArgs& a, Kind kind, int32_t B, int32_t H, in
   memcpy(&bits, &sm_scale, sizeof bits);
   if (bits == 0 || bits > 0x461c4000u)         // 1e4f; negative values, infinities and NaN are above it
     return fail(LITEVAR_E_INVALID_ARG, "sm_scale must be finite, positive and at most 1e4");
-  if (litevar_status s = strides_of(q_strides, B, H, q_len, D, a.qs)) return s;
-  if (litevar_status s = strides_of(kv_strides, B, H_kv, kv_len, D, a.ks)) return s;
-  if (litevar_status s = strides_of(o_strides, B, H, q_len, D, a.os)) return s;
+  if (litevar_status s = operand_strides(q_strides, B, H, q_len, D, a.qs)) return s;
+  if (litevar_status s = operand_strides(kv_strides, B, H_kv, kv_len, D, a.ks)) return s;
+  if (litevar_status s = operand_strides(o_strides, B, H, q_len, D, a.os)) return s;
   if (q_len == 0) return LITEVAR_OK;
   if (!a.q || !a.o || (kv_len > 0 && (!a.k || !a.v))) return fail(LITEVAR_E_INVALID_ARG, "q, k, v or o is NULL");
   if (a.o == a.q || (kv_len > 0 && (a.o == a.k || a.o == a.v))) return fail(LITEVAR_E_INVALID_ARG, "o aliases an input");

@@ -28,12 +28,6 @@ __device__ inline void unpack4(unsigned w, float (&x)[4]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) x[e] = (float)((int)(w << (24 - 8 * e)) >> 24);
 }
-__device__ inline bf16x8 codes_to_bf16(unsigned lo, unsigned hi) {
-  float a[4], b[4];
-  unpack4(lo, a); unpack4(hi, b);
-  return bf16x8{(__bf16)a[0], (__bf16)a[1], (__bf16)a[2], (__bf16)a[3], (__bf16)b[0], (__bf16)b[1], (__bf16)b[2], (__bf16)b[3]};
-}
-
 }  // namespace
 
 template <int W>

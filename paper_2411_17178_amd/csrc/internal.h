@@ -106,6 +106,10 @@ int64_t spread_over_xcds(AttnArgs& a, int64_t items, int row_bytes);
 litevar_status make_attn_args(const litevar_plan* plan, int32_t B, int32_t H, int32_t D, float sm_scale,
                               const uint8_t* d_cfg_share, uint32_t flags, AttnArgs& a);
 
+// Checks the element strides of a [B, heads, n, D] operand's first three axes and copies them; `s` NULL: packed.  (For the
+// 8-bit cache's and the cross attention's entry points.)
+litevar_status operand_strides(const int64_t* s, int B, int heads, int64_t n, int D, int64_t (&out)[3]);
+
 // The block scales of an 8-bit cache whose segments are a plan's scales: token t of segment j lies in block
 // (t + shift[j]) / 64, segment j begins at token off[j].
 struct KV8Scales {

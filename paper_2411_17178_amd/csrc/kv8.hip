@@ -257,16 +257,17 @@ Route route_of(const litevar_plan* plan) {
   return streamed <= 3 * seen ? kInKernel : kCopy;
 }
 
+}  // namespace
+
 // (the stride of an axis with one entry is never used, and is what it is)
-litevar_status check_rows(const int64_t* s, int B, int H, int64_t n, int D, int64_t (&out)[3]) {
-  if (!s) { out[2] = D; out[1] = n * D; out[0] = (int64_t)H * n * D; return LITEVAR_OK; }
-  out[0] = B > 1 ? s[0] : 0; out[1] = H > 1 ? s[1] : 0; out[2] = n > 1 ? s[2] : D;
+litevar_status operand_strides(const int64_t* s, int B, int heads, int64_t n, int D, int64_t (&out)[3]) {
+  if (!s) { out[2] = D; out[1] = n * D; out[0] = heads * n * D; return LITEVAR_OK; }
+  out[0] = B > 1 ? s[0] : 0; out[1] = heads > 1 ? s[1] : 0; out[2] = n > 1 ? s[2] : D;
   if (out[2] < D || out[2] % 8 || out[1] < 0 || out[0] < 0 || out[1] % 8 || out[0] % 8)
     return fail(LITEVAR_E_INVALID_ARG, "strides must be non-negative multiples of 8 with token stride >= D");
   return LITEVAR_OK;
 }
 
-}  // namespace
 }  // namespace lv
 
 using namespace lv;
@@ -290,7 +291,7 @@ litevar_status litevar_kv8_store(const int32_t* segments, int32_t n_segments, in
   if (dt != LITEVAR_BF16 && dt != LITEVAR_F32) return fail(LITEVAR_E_UNSUPPORTED, "unknown dtype %d", (int)dt);
   if (litevar_status s = make_blocks(segments, n_segments, segment_begin, segment_end, B, H, a.w)) return s;
   const int64_t n = a.w.off[a.w.n_seg] - a.w.off[0];
-  if (litevar_status s = check_rows(kv_strides, B, H, n, D, a.xs)) return s;
+  if (litevar_status s = operand_strides(kv_strides, B, H, n, D, a.xs)) return s;
   if (n == 0) return LITEVAR_OK;
   if (!d_k || !d_v || !d_k8 || !d_k_scale || !d_v8 || !d_v_scale) return fail(LITEVAR_E_INVALID_ARG, "a pointer is NULL");
   if (((uintptr_t)d_k | (uintptr_t)d_v | (uintptr_t)d_k8 | (uintptr_t)d_v8) & 15)
@@ -343,8 +344,8 @@ litevar_status litevar_windowed_attn_kv8_fwd(const litevar_plan* plan, const voi
   if (need > 0 && !d_workspace) return fail(LITEVAR_E_INVALID_ARG, "d_workspace is NULL");
   if (workspace_bytes < need) return fail(LITEVAR_E_INVALID_ARG, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
   if (need > 0 && ((uintptr_t)d_workspace & 255)) return fail(LITEVAR_E_INVALID_ARG, "d_workspace must be 256-byte aligned");
-  if (litevar_status s = check_rows(q_strides, B, H, plan->q_len, D, a.qs)) return s;
-  if (litevar_status s = check_rows(o_strides, B, H, plan->q_len, D, a.os)) return s;
+  if (litevar_status s = operand_strides(q_strides, B, H, plan->q_len, D, a.qs)) return s;
+  if (litevar_status s = operand_strides(o_strides, B, H, plan->q_len, D, a.os)) return s;
   if (d_o == d_q) return fail(LITEVAR_E_INVALID_ARG, "o aliases an input");
   if (((uintptr_t)d_q | (uintptr_t)d_k8 | (uintptr_t)d_v8 | (uintptr_t)d_o) & 15)
     return fail(LITEVAR_E_INVALID_ARG, "q, o and the codes must be 16-byte aligned");
