@@ -12,8 +12,8 @@
 // What a call cannot do without: Q, O and the valid keys' K and V once, 256 operations per row and key.  256 rows, 480 pairs of 77 to 512
 // keys, bf16: 22.4 us for 73 MB (14.4 at the copy rate); 2240 rows, 32 pairs, fp32: 53 us for 4.2 GFLOP (27 at a large
 // product's rate); four rows (one token, 4 query
-// heads) on up to 30 011 keys in codes, 16 pairs: 17.7 us for 44 MB (8.7); 169 rows, 480 pairs of 51 to 333
-// keys in codes: 17.5 us (7.0).
+// heads) on up to 30 011 keys in codes, 16 pairs: 17.5 us for 44 MB (8.7); 169 rows, 480 pairs of 51 to 333
+// keys in codes: 17.7 us (7.0).
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -517,7 +517,7 @@ __device__ inline void keep_part(const CrossArgs& a, int bj, int part, int n_key
 // keys that count, is added to the exponent, which costs nothing per score; the chunk's part of the row sum is divided by it
 // again.  (Relative V scales are taken as at least 2^-96, so that no probability that counts is flushed to zero.)
 //
-// 288 pairs of 2240 rows on 149 to 512 keys: 88 us (650 TFLOP/s; on 2048 keys each 870).  What bounds it there is the vector issue,
+// 288 pairs of 2240 rows on 149 to 512 keys: 88 to 92 us from card to card (650 to 624 TFLOP/s; on 2048 keys each 870).  What bounds it there is the vector issue,
 // 54 instructions and 16 exponentials for 32 rows x 32 keys, about 300 more for a tile's start and end, and Q and O, 34 us
 // at the copy rate, beside which a round of workgroups starts and ends with little else to do.  512 workgroups that stay, each with
 // a run of five or six tiles whose rows of Q come under the tile before: 102 us (the runs are uneven).

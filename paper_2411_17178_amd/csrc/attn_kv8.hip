@@ -14,9 +14,9 @@
 // key, every lane reads the eight it owns).  Scales that are not finite reach the queries that keep their keys only:
 // nothing is multiplied with a scale where the probability is zero.
 //
-// Bound: start-up (descriptor, tokens, rows, products one behind the other).  16 queries, 480 pairs 5.0 us in a graph; 25 queries
-// 7.7 with one wave per patch, 10.1 with four.  Not for longer steps: 256 queries on 680 keys 80 us, 30 with keys shared
-// through LDS.
+// Bound: start-up (descriptor, tokens, rows, products one behind the other).  16 queries, 480 pairs 5.2 us in a graph; 25 queries
+// 7.2 with one wave per patch, about 10 with four.  Every patch gathers and converts for itself: 36 / 64 queries 8.9 / 12.9 us, 5.8 / 7.9 in
+// bf16 with keys shared through LDS.  Not for longer steps: 256 queries on 680 keys 80 us, 30 shared.
 #include "attn_bf16_common.h"
 
 namespace lv {
