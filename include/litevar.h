@@ -464,7 +464,8 @@ litevar_status litevar_windowed_attn_kv8_fwd(const litevar_plan* plan, const voi
  *               probabilities ahead of their rounding to bf16.  A scale that is not finite makes NaN (an infinite one of V:
  *               infinities or NaN) of the rows that see its block.
  * Inputs must be finite; a NaN in Q, or in a row of K or V that counts, makes NaN of the results that it enters and of no
- * others.  Results do not depend on the run (no atomics).  Asynchronous on `stream`.
+ * others.  A row with keys whose scores are all -inf in fp32 is NaN.  Results do not depend on the run (no atomics).
+ * Asynchronous on `stream`.
  */
 litevar_status litevar_cross_attn_workspace_bytes(int32_t B, int32_t H, int32_t H_kv, int32_t q_len, int32_t kv_len,
                                                   size_t* out_bytes);

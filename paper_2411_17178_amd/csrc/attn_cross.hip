@@ -79,6 +79,14 @@ __device__ inline int batch_of_rank(const CrossArgs& a, int r, int& n_keys) {
 // a value that is the same in all lanes, in a scalar register
 __device__ inline float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
 
+// What a row without weights is multiplied with: zero where it has no key, NaN where all its scores are -inf in fp32.  (As
+// bits, see not_finite.)
+__device__ inline float without_weights(int n_keys) {
+  unsigned u = n_keys > 0 ? 0x7fc00000u : 0u;
+  asm volatile("" : "+v"(u));
+  return __uint_as_float(u);
+}
+
 // log2 of a value >= 0 whatever its size (the instruction takes a subnormal value for 0)
 __device__ inline float log2_of(float x) {
   return x < 0x1p-126f ? __builtin_amdgcn_logf(x * 0x1p24f) - 24.f : __builtin_amdgcn_logf(x);
@@ -370,7 +378,7 @@ void k_cross_rows(CrossArgs a, float c) {
     *(float4*)(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
     return;
   }
-  const float inv = ml.y > 0.f ? 1.f / ml.y : 0.f;       // (no key: zeros)
+  const float inv = ml.y > 0.f ? 1.f / ml.y : without_weights(n_keys);
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] *= inv;
   store_row<KIND>(a, b, j, row0 + row, dims, x);
@@ -1101,9 +1109,12 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossArgs a, float unit, flo
     for (int e = 0; e < 8; ++e) { out[e] *= inv; any += out[e]; }
     store_row<KIND>(a, b, j, r, tid, out);
   }
-  // (as in store_tile: products that only overflowed under sums that had been let grow, those of all parts together)
-  if (__builtin_expect(__builtin_amdgcn_ballot_w64(not_finite(any)) != 0, 0) && l > (float)keys_of(a, b))
-    row_again<KIND>(a, c, b, j, bj, keys_of(a, b), r);
+  // (as in store_tile: products that only overflowed under sums that had been let grow, those of all parts together; and rows whose
+  // scores are all -inf in fp32, which become NaN there)
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(not_finite(any) || l == 0.f) != 0, 0)) {
+    const int n_keys = keys_of(a, b);
+    if (n_keys > 0 && (l == 0.f || l > (float)n_keys)) row_again<KIND>(a, c, b, j, bj, n_keys, r);
+  }
 }
 
 namespace {

@@ -178,3 +178,21 @@ def test_an_infinite_k_scale_under_negative_products(lv, shape):
     want, tol = _reference("codes", q, k, v)
     cache.k_scale[0, 0, 1] = INF
     _check(lv.litevar_cross_attn_kv8_fwd(q, cache, SM), want, tol, _hit(shape))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "codes"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_rows_whose_scores_all_lie_below_the_range_are_nan(lv, shape, kind):
+    """fp32 does not hold their weights: NaN in every kernel, not the zeros of a row without keys, which the last batch row has."""
+    B, H, Hkv, n, L = shape
+    q, k, v = (x.float() for x in _operands(shape, "bf16"))
+    q[..., 0], k[..., 0] = 2.0 ** 70, -2.0 ** 70
+    lens = torch.full((B,), L, dtype=torch.int32, device="cuda")
+    lens[-1] = 0
+    if kind == "codes":
+        cache = lv.litevar_kv8_store(lv.litevar_kv8_cache([L], B, Hkv), k, v)
+        out = lv.litevar_cross_attn_kv8_fwd(q.to(torch.bfloat16), cache, SM, lens=lens)
+    else:
+        dtype = torch.float32 if kind == "f32" else torch.bfloat16
+        out = lv.litevar_cross_attn_fwd(*(x.to(dtype) for x in (q, k, v)), SM, lens=lens)
+    assert bool(torch.isnan(out[:-1]).all()) and bool((out[-1] == 0).all())
